@@ -53,7 +53,11 @@
 extern "C" {
 #endif
 
-typedef enum { SG_F32 = 0, SG_BF16 = 1 } sg_dtype;
+typedef enum {
+  SG_F32 = 0,
+  SG_BF16 = 1,
+  SG_F8_E4M3 = 2 /* 8 bits, 4 of exponent, 3 of mantissa, largest 448, no infinity: an output of sg_tile_residual_norm */
+} sg_dtype;
 
 typedef enum {
   SG_OK = 0,
@@ -425,6 +429,103 @@ int sg_refine_step(const sg_problem* p, const sg_gain_step_io* io, const sg_regi
 int sg_refine_step_canvas(const sg_problem* p, const void* q, const void* k, const void* v, void* const* tile_x,
                           const sg_gain_step_io* io, const sg_region_control* region,
                           const sg_scheduler_update* update, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The rest of a tile's transformer block that needs the device's own kernels (Algorithm 1 "Model.DiT"; the projections
+ * between them are the caller's matrix products): attention to tokens beside the tile's own, and the norm of its residual
+ * stream.  All of them take the tiles as host arrays of device pointers and, like the cached step, skip the tiles whose run
+ * flag is 0 on the device; such a tile's outputs are left as they are.
+ *
+ * sg_context_problem: the shapes of one attention call.  Element c of head a of token n of a tensor lies at
+ *     base + a*stride_head + n*stride_token + c      (in elements)
+ * so that [heads][tokens][d] and [tokens][heads][d] (what a projection leaves) are both expressible.  Keys and values of one
+ * segment share their strides (those of a segment of 0 tokens are not looked at).  All strides are positive multiples of 8,
+ * stride_token >= head_dim and below 2^22 for keys; heads * tokens is below 2^25; base pointers are 16-byte aligned. */
+typedef struct sg_context_problem {
+  int32_t heads, kv_heads;    /* heads of the queries; of keys and values: a divisor of heads (head a reads a / (heads / kv_heads)) */
+  int32_t head_dim;           /* 64 or 128                                                                       */
+  int32_t dtype;              /* SG_F32 or SG_BF16, of every tensor                                              */
+  float scale;                /* softmax scale, > 0 (1/sqrt(head_dim))                                           */
+  int32_t tokens;             /* queries of a tile, >= 1                                                         */
+  int32_t ctx_tokens;         /* rows that the context's (prefix's) buffers hold, >= 0                           */
+  int32_t own_tokens;         /* prefix attention: rows that a tile's own buffers hold, >= 0                     */
+  int64_t q_stride_token, q_stride_head;
+  int64_t ctx_stride_token, ctx_stride_head;   /* keys and values of the context / prefix                        */
+  int64_t own_stride_token, own_stride_head;   /* a tile's own keys and values                                   */
+  int64_t out_stride_token, out_stride_head;   /* no two elements of an output may share a place                 */
+} sg_context_problem;
+
+/* Checks a context problem (host only, launches nothing). */
+int sg_context_validate(const sg_context_problem* p);
+
+/* Bytes of device scratch that the two calls below need for n_tiles tiles (the larger of the two; it may be 0).  The
+ * workspace is 256-byte aligned device memory; it needs no initialisation and may be reused by the next call on the same
+ * stream.  Two calls that may run at the same time (streams, graphs) need a workspace each. */
+int sg_context_workspace_bytes(const sg_context_problem* p, int32_t n_tiles, size_t* out_bytes);
+
+/*
+ * Cross attention of tiles to an encoder's states.  For tile i, head a and query n:
+ *     O[a][n][:] = sum_m softmax_m( scale * <Q[a][n], K[a'][m]> ) * V[a'][m][:],   a' = a / (heads / kv_heads)
+ * over the places m < ctx_len[i] of tile i's context with key_mask[i][m] != 0.  A query without any such place, or whose
+ * scores are all -inf, gives zeros.  Keys and values at other places are not read: they may hold anything.
+ *   q, out     host arrays of n_tiles device pointers: queries and outputs of a tile
+ *   k, v       host arrays of n_tiles device pointers: the context of each tile; tiles with the same prompt name the same
+ *              buffers.  With ctx_tokens = 0 they are not looked at (NULL is fine)
+ *   ctx_len    device, n_tiles lengths (outside 0 .. ctx_tokens: the nearer of the two), or NULL: ctx_tokens each
+ *   key_mask   device, [n_tiles][ctx_tokens] bytes, 0 = the place does not count, or NULL
+ *   run        device, n_tiles bytes (sg_cache_gate's recompute), or NULL: all tiles
+ * bf16 problems multiply in bf16 on the matrix cores (probabilities are rounded to bf16 for the second product), accumulate
+ * in fp32 and scale the scores in fp32 behind the product; f32 problems multiply and accumulate in fp32.  A NaN in Q, or at a
+ * place that counts in K or V, reaches every output that depends on it, and no other.  Tiles are attended up to 64 a launch; calls with
+ * few queries are cut along the keys and joined by a second launch.  The same call gives the same bits every time.
+ */
+int sg_tile_cross_attention(const sg_context_problem* p, int32_t n_tiles, const void* const* q, const void* const* k,
+                            const void* const* v, const int32_t* ctx_len, const uint8_t* key_mask, const uint8_t* run,
+                            void* const* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of tiles to a prefix that all of them share and to keys of their own, in one softmax: the joint attention of text and
+ * tile (prefix = the text's tokens, own = the tile's: own_tokens = tokens), tiles that all see the tokens of a sketch of the whole canvas, or
+ * single tokens of many requests behind one long prompt.  For tile i:
+ *     O[a][n][:] = sum_m softmax_m( scale * <Q[a][n], K[a'][m]> ) * V[a'][m][:]
+ * over the prefix_len places of the prefix and the own_len[i] places of tile i's own k and v.  No place: zeros.
+ *   prefix_k, prefix_v  device; with ctx_tokens = 0 not looked at
+ *   k, v                host arrays of n_tiles device pointers; with own_tokens = 0 not looked at
+ *   own_len             device, n_tiles lengths, or NULL: own_tokens each;  prefix_len: device, one length, or NULL: ctx_tokens
+ * Everything else as sg_tile_cross_attention.  Where a tile has at most 16 queries per head of keys, those of all tiles (of a launch)
+ * are stacked and the prefix is read once for all of them.
+ */
+int sg_tile_prefix_attention(const sg_context_problem* p, int32_t n_tiles, const void* const* q, const void* const* k,
+                             const void* const* v, const void* prefix_k, const void* prefix_v, const int32_t* own_len,
+                             const int32_t* prefix_len, const uint8_t* run, void* const* out, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Shapes of a residual norm: rows x channels per tile; row n of a tensor begins at base + n*stride (elements). */
+typedef struct sg_norm_problem {
+  int32_t rows;               /* per tile, >= 0                                                                  */
+  int32_t channels;           /* a multiple of 8, 8 .. 32768                                                     */
+  int32_t dtype;              /* SG_F32 or SG_BF16: x, residual, weight, sum                                     */
+  int32_t out_dtype;          /* dtype, or SG_F8_E4M3                                                            */
+  int32_t scale_group;        /* SG_F8_E4M3: channels that share a scale: 0 = the whole row, or 128 (a divisor of channels) */
+  float eps;                  /* >= 0                                                                            */
+  int64_t x_stride, residual_stride, sum_stride, out_stride;   /* multiples of 8, >= channels                     */
+} sg_norm_problem;
+
+/*
+ * Residual addition and root-mean-square norm:  s = x + residual,  y = s * rsqrt(mean(s^2) + eps) * weight  per row.
+ *   residual   host array of n_tiles device pointers, or NULL: s = x
+ *   weight     device, `channels` elements, or NULL: ones
+ *   sum        host array: s in the tensors' type, or NULL.  sum[i] may be x[i] or residual[i] (with its stride): in place
+ *   out        host array: y in the tensors' type; or, with SG_F8_E4M3, y / scale rounded to 8 bits, scale = max|y| / 448 over a
+ *              row or over each 128 channels of it (0 where that maximum is below 2^-100: zeros are written).  Aliases nothing
+ *   out_scale  SG_F8_E4M3: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats; else NULL
+ *   run        device, n_tiles bytes, or NULL: all tiles
+ * y is computed from the sum before it is rounded, in fp32; |s| below 2^60 (the squares are summed in fp32).  A row with a NaN is
+ * NaN throughout.  All pointers 16-byte aligned (out_scale: 4).
+ */
+int sg_tile_residual_norm(const sg_norm_problem* p, int32_t n_tiles, const void* const* x, const void* const* residual,
+                          const void* weight, const uint8_t* run, void* const* sum, void* const* out,
+                          float* const* out_scale, void* stream);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,7 @@ been built, loading raises.
 import ctypes
 import os
 
-SG_F32, SG_BF16 = 0, 1
+SG_F32, SG_BF16, SG_F8_E4M3 = 0, 1, 2
 SG_OK, SG_ERR_INVALID_ARG, SG_ERR_UNSUPPORTED, SG_ERR_WORKSPACE, SG_ERR_HIP = 0, -1, -2, -3, -4
 SG_REGION_MAXMIN, SG_REGION_TOPSELECT = 0, 1
 SG_STATIC_GATE_MAX_TILES = 64
@@ -77,6 +77,23 @@ class sg_scheduler_update(ctypes.Structure):
                 ("c_latent", ctypes.c_float), ("c_noise", ctypes.c_float)]
 
 
+class sg_context_problem(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float),
+                ("tokens", ctypes.c_int32), ("ctx_tokens", ctypes.c_int32), ("own_tokens", ctypes.c_int32),
+                ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("ctx_stride_token", ctypes.c_int64), ("ctx_stride_head", ctypes.c_int64),
+                ("own_stride_token", ctypes.c_int64), ("own_stride_head", ctypes.c_int64),
+                ("out_stride_token", ctypes.c_int64), ("out_stride_head", ctypes.c_int64)]
+
+
+class sg_norm_problem(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("channels", ctypes.c_int32), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("scale_group", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("sum_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64)]
+
+
 def library_path():
     return os.path.join(_PKG, "libsupergen_tile.so")
 
@@ -141,6 +158,17 @@ def load_library():
     lib.sg_tile_similarity.argtypes = [pp, pp, i32, i64, i32, vp, vp, vp, ctypes.c_size_t, vp]
     lib.sg_region_thresholds.restype = ctypes.c_int
     lib.sg_region_thresholds.argtypes = [vp, vp, vp, i32, f32, f32, i32, i32, vp, vp, vp]
+    ctx = ctypes.POINTER(sg_context_problem)
+    lib.sg_context_validate.restype = ctypes.c_int
+    lib.sg_context_validate.argtypes = [ctx]
+    lib.sg_context_workspace_bytes.restype = ctypes.c_int
+    lib.sg_context_workspace_bytes.argtypes = [ctx, i32, ctypes.POINTER(ctypes.c_size_t)]
+    lib.sg_tile_cross_attention.restype = ctypes.c_int
+    lib.sg_tile_cross_attention.argtypes = [ctx, i32, pp, pp, pp, vp, vp, vp, pp, vp, ctypes.c_size_t, vp]
+    lib.sg_tile_prefix_attention.restype = ctypes.c_int
+    lib.sg_tile_prefix_attention.argtypes = [ctx, i32, pp, pp, pp, vp, vp, vp, vp, vp, pp, vp, ctypes.c_size_t, vp]
+    lib.sg_tile_residual_norm.restype = ctypes.c_int
+    lib.sg_tile_residual_norm.argtypes = [ctypes.POINTER(sg_norm_problem), i32, pp, pp, vp, vp, pp, pp, pp, vp]
     _LIB = lib
     return lib
 
@@ -460,3 +488,70 @@ def sg_region_thresholds(tile_std, track_mean, track_count, tau_base, alpha, mod
                                              _stream())
     _check(rc, "sg_region_thresholds")
     return thresholds
+
+
+# ------------------------------------------------------------------ the rest of a tile's block: context attention, residual norm
+_DTYPES = {"f32": SG_F32, "bf16": SG_BF16, "e4m3": SG_F8_E4M3, SG_F32: SG_F32, SG_BF16: SG_BF16, SG_F8_E4M3: SG_F8_E4M3}
+
+
+def make_context_problem(tokens, ctx_tokens, heads, head_dim, dtype, kv_heads=None, own_tokens=0, scale=None, token_major=False):
+    """sg_context_problem of packed tensors: [heads][tokens][d], or [tokens][heads][d] if token_major.  Other strides: set the fields."""
+    kv = heads if kv_heads is None else kv_heads
+    p = sg_context_problem(heads=int(heads), kv_heads=int(kv), head_dim=int(head_dim), dtype=_DTYPES[dtype],
+                           scale=float(head_dim ** -0.5 if scale is None else scale), tokens=int(tokens),
+                           ctx_tokens=int(ctx_tokens), own_tokens=int(own_tokens))
+    for name, a, n in (("q", heads, tokens), ("ctx", kv, ctx_tokens), ("own", kv, own_tokens), ("out", heads, tokens)):
+        setattr(p, name + "_stride_token", int(a) * int(head_dim) if token_major else int(head_dim))
+        setattr(p, name + "_stride_head", int(head_dim) if token_major else max(1, int(n)) * int(head_dim))
+    return p
+
+
+def sg_context_validate(p):
+    return load_library().sg_context_validate(ctypes.byref(p))
+
+
+def sg_context_workspace_bytes(p, n_tiles):
+    out = ctypes.c_size_t(0)
+    _check(load_library().sg_context_workspace_bytes(ctypes.byref(p), int(n_tiles), ctypes.byref(out)), "sg_context_workspace_bytes")
+    return out.value
+
+
+def _scratch(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def _pointers(tensors):
+    """_ptr_array, or NULL for no list."""
+    return None if tensors is None else _ptr_array(tensors)
+
+
+def sg_tile_cross_attention(p, q, k, v, out, ctx_len=None, key_mask=None, run=None, workspace=None):
+    """q, k, v, out: lists of one tensor per tile (k, v: None if the context has no tokens); ctx_len: int32, key_mask and run: uint8."""
+    st = load_library().sg_tile_cross_attention(ctypes.byref(p), len(q), _ptr_array(q), _pointers(k), _pointers(v), _ptr(ctx_len),
+                                                _ptr(key_mask), _ptr(run), _ptr_array(out), *_scratch(workspace), _stream())
+    _check(st, "sg_tile_cross_attention")
+    return out
+
+
+def sg_tile_prefix_attention(p, q, k, v, prefix_k, prefix_v, out, own_len=None, prefix_len=None, run=None, workspace=None):
+    """q, k, v, out: lists of one tensor per tile (k, v: None if tiles have no keys of their own); own_len, prefix_len: int32; run: uint8."""
+    st = load_library().sg_tile_prefix_attention(ctypes.byref(p), len(q), _ptr_array(q), _pointers(k), _pointers(v), _ptr(prefix_k),
+                                                 _ptr(prefix_v), _ptr(own_len), _ptr(prefix_len), _ptr(run), _ptr_array(out),
+                                                 *_scratch(workspace), _stream())
+    _check(st, "sg_tile_prefix_attention")
+    return out
+
+
+def make_norm_problem(rows, channels, dtype, out_dtype=None, scale_group=0, eps=1e-6):
+    """sg_norm_problem of packed rows; other strides: set the fields.  out_dtype: None (as dtype) or "e4m3"."""
+    c = int(channels)
+    return sg_norm_problem(rows=int(rows), channels=c, dtype=_DTYPES[dtype], out_dtype=_DTYPES[dtype if out_dtype is None else out_dtype],
+                           scale_group=int(scale_group), eps=float(eps), x_stride=c, residual_stride=c, sum_stride=c, out_stride=c)
+
+
+def sg_tile_residual_norm(p, x, weight, out, residual=None, sum_out=None, out_scale=None, run=None):
+    """x, out, residual, sum_out, out_scale: lists of one tensor per tile, the last three or None; weight: `channels` elements or None."""
+    st = load_library().sg_tile_residual_norm(ctypes.byref(p), len(x), _ptr_array(x), _pointers(residual), _ptr(weight), _ptr(run),
+                                              _pointers(sum_out), _ptr_array(out), _pointers(out_scale), _stream())
+    _check(st, "sg_tile_residual_norm")
+    return out

@@ -1,0 +1,441 @@
+// Attention of tiles to tokens beside their own (sg_tile_cross_attention, sg_tile_prefix_attention), bf16: products on the matrix
+// cores with fp32 accumulation, softmax in fp32 against the true running maximum, scores scaled in fp32 behind the product.
+//
+// Both kernels form S^T = K Q^T, which puts one row (query) per lane column, so that the probabilities of a row stay in their lanes
+// and are already the B operand of O^T = V^T P^T; V^T comes out of LDS through the transposing read.
+//
+//   context_bf16_wide_kernel   calls with rows to fill the chip: 128 rows share every 64 keys through LDS, both segments in one pass
+//   context_bf16_split_kernel  calls with few rows: every wavefront streams keys of its own through LDS of its own, 32 rows at a time,
+//                              and the shares of a row are joined in LDS and, over workgroups, by the join kernel
+#include <atomic>
+#include "context_common.h"
+
+namespace sg {
+namespace {
+
+#define SG_INLINE __attribute__((always_inline))
+
+constexpr int kSlot = 256;   // LDS bytes of a "slot": one key of head_dim 128, two neighbouring ones of head_dim 64
+
+__device__ __forceinline__ f32x16 zero16() {
+  return f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+}
+
+// Per-lane LDS offsets of the fragments.  16-byte chunk c of K slot r sits at chunk c ^ (r & 15), of V slot r at c ^ ((r & 3) << 2):
+// both reads are then free of bank conflicts.
+struct Frags {
+  uint32_t k[8];   // slot lq, chunk 2 kk + half
+  uint32_t v[4];   // transposing read: 64-byte piece db of 4 slots
+};
+__device__ __forceinline__ Frags make_frags() {
+  const int lane = threadIdx.x & 63, lq = lane & 31, half = lane >> 5;
+  Frags f;
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) f.k[kk] = lq * kSlot + (((2 * kk + half) ^ (lq & 15)) << 4);
+  const int grp = lane >> 4, gi = lane & 15;
+  const int row = 4 * (grp >> 1) + (gi >> 2), dbyte = (16 * (grp & 1) + 4 * (gi & 3)) * 2;
+#pragma unroll
+  for (int db = 0; db < 4; ++db) f.v[db] = row * kSlot + (((4 * db + (dbyte >> 4)) ^ ((row & 3) << 2)) << 4) + (dbyte & 15);
+  return f;
+}
+
+// One row's softmax (the same in lanes l and l ^ 32) and its output accumulators.
+template <int D>
+struct RowState {
+  f32x16 o[D / 32];
+  float m;   // running maximum, log2 domain
+  float l;   // this lane's share of the sum
+};
+template <int D>
+__device__ __forceinline__ void clear(RowState<D>& st) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
+  st.m = -__builtin_inff();
+  st.l = 0.f;
+}
+
+// NB blocks of 32 keys, K at LDS address kb0 and V at vb0.  head_dim 128: block b is the slots 32 b .. 32 b + 31; head_dim 64: the 32 slots
+// hold two keys each and block b (of 2) is their b-th ones.  Register r of a block is row 8 (r >> 2) + 4 half + (r & 3) of it.
+// valid: bit i = key i of these counts.
+template <int D, int NB>
+__device__ __forceinline__ void attend_keys(const Frags& f, const uint32_t kb0, const uint32_t vb0, const bf16x8 (&qf)[D / 16], const float c_log2,
+                                            const uint64_t valid, RowState<D>& st) {
+  static_assert(D == 128 || NB == 2, "");
+  constexpr uint64_t kFull = (D == 128 && NB == 1) ? 0xffffffffull : ~0ull;
+  const int half = (threadIdx.x & 63) >> 5;
+  f32x16 s[NB];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const uint32_t at = kb0 + f.k[D == 128 ? kk : 4 * b + kk] + (D == 128 ? b * 32 * kSlot : 0);
+      const bf16x8 x = __builtin_bit_cast(bf16x8, *(const SG_LDS u32x4*)(uintptr_t)at);
+      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[kk], kk == 0 ? zero16() : s[b], 0, 0, 0);
+    }
+  if (valid != kFull) {   // scores of the keys that do not count become -inf
+    const uint64_t mine = valid >> (D == 128 ? 4 * half : 8 * half);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = 8 * (r >> 2) + (r & 3), bit = D == 128 ? 32 * b + row : 2 * row + b;
+        const uint32_t w = bit < 32 ? (uint32_t)mine : (uint32_t)(mine >> 32);
+        const uint32_t keep = (uint32_t)((int32_t)(w << (31 - (bit & 31))) >> 31);
+        s[b][r] = __uint_as_float((__float_as_uint(s[b][r]) & keep) | (0xff800000u & ~keep));
+      }
+  }
+  float mx = s[0][0];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+  const uint32_t mu = __float_as_uint(mx);
+  const auto sw = __builtin_amdgcn_permlane32_swap(mu, mu, false, false);
+  mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  const float top = fmaxf(st.m, mx * c_log2);
+  if (__any(top != st.m)) {
+    const float alpha = st.m == top ? 1.f : __builtin_amdgcn_exp2f(st.m - top);   // first keys: exp2(-inf) = 0
+    st.m = top;
+    st.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) st.o[db] *= alpha;
+  }
+  const float ref = st.m == -__builtin_inff() ? 0.f : st.m;   // no key so far: probabilities 0
+  // The probabilities are rounded to bf16 for the second product (2^-9 of each, which averages out over a row); their sum is taken before.
+  float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 p;
+#pragma unroll
+      for (int r = 0; r < 8; r += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], c_log2, -ref));
+        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r + 1], c_log2, -ref));
+        sum0 += e0;
+        sum1 += e1;
+        p[r] = (__bf16)e0;
+        p[r + 1] = (__bf16)e1;
+      }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const uint32_t at = vb0 + f.v[D == 128 ? db : 2 * b + db] + (D == 128 ? b * 32 * kSlot : 0) + h * 16 * kSlot;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)(at + 8 * kSlot));
+        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p, st.o[db], 0, 0, 0);
+      }
+    }
+  st.l += sum0 + sum1;
+}
+
+template <int D>
+__device__ __forceinline__ void load_query(const CtxArgs& a, const CtxTable& tab, const CtxRow& row, bf16x8 (&qf)[D / 16]) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const uint16_t* const q = (const uint16_t*)tab.q[row.tile] + (int64_t)row.head * a.q_head + (int64_t)row.token * a.q_token;
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) {
+    u32x4 x = *(const u32x4*)(q + 16 * kk + 8 * half);
+    if (!row.there) x = u32x4{0, 0, 0, 0};
+    qf[kk] = __builtin_bit_cast(bf16x8, x);
+  }
+}
+
+// The keys of one segment as a stage of 64 (or 32) is taken from them.
+struct Segment {
+  const char* k;    // head's first key
+  const char* v;
+  uint32_t token;   // bytes between keys
+  int len;
+  const uint8_t* mask;
+};
+__device__ __forceinline__ Segment segment(const CtxArgs& a, const CtxTable& tab, int which, int tile, int kvh) {
+  Segment g;
+  const void* const k = which == 0 ? a.k0 : tab.k[tile];
+  const void* const v = which == 0 ? a.v0 : tab.v[tile];
+  const int64_t head = (int64_t)kvh * a.kv_head[which] * 2;
+  g.k = (const char*)k + head;
+  g.v = (const char*)v + head;
+  g.token = (uint32_t)(a.kv_token[which] * 2);
+  g.len = which == 0 ? ctx_length(a.len0, 0, a.cap0) : ctx_length(a.len1, tile, a.cap1);
+  g.mask = (which == 1 && a.mask1) ? a.mask1 + (int64_t)tile * a.cap1 : nullptr;
+  return g;
+}
+// Transfers of a wavefront: instruction u moves the slots first + 4 u .. + 3; lane l fills chunk l & 15 of the (l >> 4)-th of them and
+// so fetches the chunk that belongs there: chunk `chunk` of the key `key` behind the first key of these slots.
+template <int D>
+__device__ __forceinline__ void lane_source(int slot, int lane, bool is_v, int& key, int& chunk) {
+  const int c = (lane & 15) ^ (is_v ? (slot & 3) << 2 : slot & 15);
+  key = D == 128 ? slot : 2 * slot + (c >> 3);
+  chunk = D == 128 ? c : c & 7;
+}
+// Moves N_INSTR x 4 slots of K and V, from slot `first` of a stage whose first key is key0, to LDS k_dst and v_dst.
+template <int D, int N_INSTR>
+__device__ __forceinline__ void move_keys(const Segment& g, const int key0, const int first, const uint64_t valid, const bool whole,
+                                          const uint32_t k_dst, const uint32_t v_dst) {
+  const int lane = threadIdx.x & 63;
+  const char* const kp = g.k + (int64_t)key0 * g.token;
+  const char* const vp = g.v + (int64_t)key0 * g.token;
+  if (whole) {   // 64-bit base of the stage, 32-bit offsets inside it
+#pragma unroll
+    for (int u = 0; u < N_INSTR; ++u) {
+      int kk, kc, vk, vc;
+      lane_source<D>(first + 4 * u + (lane >> 4), lane, false, kk, kc);
+      lane_source<D>(first + 4 * u + (lane >> 4), lane, true, vk, vc);
+      dma16(kp, (uint32_t)kk * g.token + (uint32_t)kc * 16, k_dst + u * 1024);
+      dma16(vp, (uint32_t)vk * g.token + (uint32_t)vc * 16, v_dst + u * 1024);
+    }
+  } else {       // keys that do not count are read from the zeros
+    const char* const zeros = (const char*)g_ctx_zeros;
+#pragma unroll
+    for (int u = 0; u < N_INSTR; ++u) {
+      int kk, kc, vk, vc;
+      lane_source<D>(first + 4 * u + (lane >> 4), lane, false, kk, kc);
+      lane_source<D>(first + 4 * u + (lane >> 4), lane, true, vk, vc);
+      dma16_addr((valid >> kk) & 1 ? kp + ((uint32_t)kk * g.token + (uint32_t)kc * 16) : zeros + kc * 16, k_dst + u * 1024);
+      dma16_addr((valid >> vk) & 1 ? vp + ((uint32_t)vk * g.token + (uint32_t)vc * 16) : zeros + vc * 16, v_dst + u * 1024);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------ few rows
+// A wavefront's LDS: two stages of 32 slots of K and V.  After the keys it holds the wavefront's sums: 32 rows x D floats (16-byte chunk c of
+// row r at chunk c ^ r), then (reference, sum) of the rows.
+constexpr int kSplitStage = 2 * 32 * kSlot;              // 16 KiB
+constexpr int kSplitWave = 2 * kSplitStage;
+constexpr int kSplitLds = 4 * kSplitWave;
+constexpr int kSumsAt = kSplitStage;
+
+template <int D>
+__global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArgs a, const CtxTable tab) {
+  constexpr int kKeys = D == 128 ? 32 : 64, kBlocks = D == 128 ? 1 : 2;
+  constexpr uint64_t kFull = kKeys == 32 ? 0xffffffffull : ~0ull;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lq = lane & 31, half = lane >> 5;
+
+  const int grid0 = (a.part[0].items + 7) / 8 * 8;
+  const int which = (int)blockIdx.x < grid0 ? 0 : 1;
+  const CtxPart& p = a.part[which];
+  int id = ctx_xcd_order((int)blockIdx.x - (which ? grid0 : 0), p.items);
+  if (id < 0) return;
+  const int row_block = id % p.row_blocks;
+  id /= p.row_blocks;
+  const int split = id % p.splits;
+  id /= p.splits;
+  const int kvh = id % a.kv_heads, batch = id / a.kv_heads;
+  if (!p.stacked && a.run && a.run[batch] == 0) return;
+  const int way = wave & (p.ways - 1);
+  const int row0 = (row_block * (4 / p.ways) + wave / p.ways) * 32;
+
+  RowState<D> st;
+  clear(st);
+  if (row0 < p.rows) {
+    const Segment g0 = segment(a, tab, 0, batch, kvh), g1 = segment(a, tab, 1, batch, kvh);
+    const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
+    const int n = n0 + n1;
+    const int from = (int)((int64_t)n * split / p.splits), to = (int)((int64_t)n * (split + 1) / p.splits);
+    const uint32_t ring = lds0 + wave * kSplitWave;
+    uint64_t valid_next = 0;
+    auto issue = [&](int j, int at) SG_INLINE {
+      const bool second = j >= n0;
+      const Segment& g = second ? g1 : g0;
+      const int key0 = (second ? j - n0 : j) * kKeys;
+      bool counts = lane < kKeys && key0 + lane < g.len;
+      if (g.mask && counts) counts = g.mask[key0 + lane] != 0;
+      const uint64_t v = __ballot(counts);
+      valid_next = v;
+      const uint32_t dst = ring + at * kSplitStage;
+      move_keys<D, 8>(g, key0, 0, v, v == kFull, dst, dst + 32 * kSlot);
+    };
+    int j = from + way;
+    if (j < to) issue(j, 0);
+    bf16x8 qf[D / 16];
+    load_query<D>(a, tab, ctx_row(a, p, batch, kvh, row0 + lq), qf);
+    const Frags f = make_frags();
+    const float c_log2 = a.scale * 1.4426950408889634f;
+    for (int at = 0; j < to; j += p.ways, at ^= 1) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // this stage is there, the other one has been read
+      __builtin_amdgcn_sched_barrier(0);
+      const uint64_t v = valid_next;
+      if (j + p.ways < to) issue(j + p.ways, at ^ 1);
+      const uint32_t base = ring + at * kSplitStage;
+      if (v != 0) attend_keys<D, kBlocks>(f, base, base + 32 * kSlot, qf, c_log2, v, st);
+    }
+  }
+  const uint32_t lu = __float_as_uint(st.l);
+  const auto sw = __builtin_amdgcn_permlane32_swap(lu, lu, false, false);
+  const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+
+  // ---- join of the shares in this workgroup
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  const uint32_t mine = lds0 + wave * kSplitWave;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 x = {st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
+      *(SG_LDS f32x4*)(uintptr_t)(mine + lq * (D * 4) + (((8 * db + 2 * g + half) ^ (lq & (D / 4 - 1))) << 4)) = x;
+    }
+  if (half == 0) *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + lq * 8) = f32x2{st.m, l};
+  __syncthreads();
+  const uint32_t group = lds0 + (wave & ~(p.ways - 1)) * kSplitWave;
+  constexpr int kLanes = D / 4;   // lanes per row: 4 channels each
+  const int rows_at_once = 64 * p.ways / kLanes, tg = way * 64 + lane;
+  const int chunk = tg % kLanes;
+  for (int r = tg / kLanes; r < 32; r += rows_at_once) {
+    if (row0 + r >= p.rows) break;
+    const CtxRow row = ctx_row(a, p, batch, kvh, row0 + r);
+    if (!row.there) continue;
+    float top = -__builtin_inff();
+    for (int w = 0; w < p.ways; ++w) top = fmaxf(top, (*(const SG_LDS f32x2*)(uintptr_t)(group + w * kSplitWave + kSumsAt + r * 8))[0]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int w = 0; w < p.ways; ++w) {
+      const uint32_t at = group + w * kSplitWave;
+      const f32x2 ml = *(const SG_LDS f32x2*)(uintptr_t)(at + kSumsAt + r * 8);
+      if (ml[1] == 0.f) continue;   // a share without keys (one whose scores are NaN has a reference of -inf too)
+      const float e = __builtin_amdgcn_exp2f(ml[0] - top);
+      sum += e * ml[1];
+      acc += e * *(const SG_LDS f32x4*)(uintptr_t)(at + r * (D * 4) + ((chunk ^ (r & (D / 4 - 1))) << 4));
+    }
+    if (a.n_shares == 1) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint16_t* const o = (uint16_t*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 4 * chunk;
+      *(u32x2*)o = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+    } else {
+      const int64_t at = (int64_t)row.rid * a.n_shares + p.first_share + split;
+      const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
+      *(f32x4*)(a.shares + at * D + 4 * chunk) = acc;
+      if (chunk == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{top, sum};
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------ many rows
+// 4 wavefronts of 32 rows share stages of 64 keys, two of them in LDS: one is attended while the next one arrives.  Two workgroups
+// of head_dim 128 fit a compute unit (64 KiB of LDS each), and the softmax of one runs beside the products of the other.
+template <int D>
+constexpr int kWideSlots = D == 128 ? 64 : 32;
+template <int D>
+constexpr int kWideStage = 2 * kWideSlots<D> * kSlot;   // K and V
+template <int D>
+constexpr int kWideLds = 2 * kWideStage<D>;
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs a, const CtxTable tab) {
+  constexpr int kKeys = 64, kInstr = kWideSlots<D> / 16, kV = kWideSlots<D> * kSlot;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lq = lane & 31, half = lane >> 5;
+  const CtxPart& p = a.part[0];
+  // Only the tiles that run are numbered, so that the work is spread evenly whichever they are.
+  uint64_t active = a.n_tiles >= 64 ? ~0ull : (1ull << a.n_tiles) - 1;
+  if (a.run) active = __ballot(lane < a.n_tiles && a.run[lane < a.n_tiles ? lane : 0] != 0);
+  const int per_tile = a.kv_heads * p.row_blocks;
+  const int id = ctx_xcd_order((int)blockIdx.x, __builtin_popcountll(active) * per_tile);
+  if (id < 0) return;
+  const int nth = id / per_tile, in_tile = id - nth * per_tile;
+  const int tile = __builtin_amdgcn_readfirstlane(ctx_nth_tile(active, nth));
+  const int kvh = __builtin_amdgcn_readfirstlane(in_tile / p.row_blocks), row_block = in_tile - kvh * p.row_blocks;
+  const int row0 = row_block * 128 + wave * 32;
+
+  const Segment g0 = segment(a, tab, 0, tile, kvh), g1 = segment(a, tab, 1, tile, kvh);
+  const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
+  const int n = n0 + n1;
+  uint64_t valid = 0, valid_next = 0;
+  bool mask_next = true;   // of the stage that is issued next: whether key key0 + lane is unmasked
+  auto fetch_mask = [&](int j) SG_INLINE {
+    const int key = (j - n0) * kKeys + lane;
+    mask_next = !(j >= n0 && j < n && g1.mask) || (key < g1.len && g1.mask[key] != 0);
+  };
+  auto issue = [&](int j) SG_INLINE {
+    const bool second = j >= n0;
+    const Segment& g = second ? g1 : g0;
+    const int key0 = (second ? j - n0 : j) * kKeys;
+    valid_next = __ballot(mask_next && key0 + lane < g.len);
+    const int first = wave * (kWideSlots<D> / 4);
+    const uint32_t dst = lds0 + (j & 1) * kWideStage<D> + first * kSlot;
+    move_keys<D, kInstr>(g, key0, first, valid_next, valid_next == ~0ull, dst, dst + kV);
+    if (g1.mask) fetch_mask(j + 1);
+  };
+  if (n > 0) {
+    if (g1.mask) fetch_mask(0);
+    issue(0);
+  }
+  bf16x8 qf[D / 16];
+  load_query<D>(a, tab, ctx_row(a, p, tile, kvh, row0 + lq), qf);
+  const Frags f = make_frags();
+  const float c_log2 = a.scale * 1.4426950408889634f;
+  RowState<D> st;
+  clear(st);
+  for (int j = 0; j < n; ++j) {
+    // own transfers of stage j have landed, everyone's behind the barrier, where nobody reads the other stage any more
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    valid = valid_next;
+    if (j + 1 < n) issue(j + 1);
+    const uint32_t base = lds0 + (j & 1) * kWideStage<D>;
+    if (valid != 0) attend_keys<D, 2>(f, base, base + kV, qf, c_log2, valid, st);
+  }
+  // ---- rows go out through LDS (8 KiB a wavefront), so that a store writes whole rows; chunk c of row r sits at chunk c ^ (r % kChunks)
+  constexpr int kChunks = D / 8, kRowsPer = 64 / kChunks;
+  const uint32_t lu = __float_as_uint(st.l);
+  const auto sw = __builtin_amdgcn_permlane32_swap(lu, lu, false, false);
+  const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  const uint32_t buf = lds0 + wave * (32 * D * 2);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const u32x2 w = {pack_bf16x2(st.o[db][4 * g] * inv, st.o[db][4 * g + 1] * inv), pack_bf16x2(st.o[db][4 * g + 2] * inv, st.o[db][4 * g + 3] * inv)};
+      *(SG_LDS u32x2*)(uintptr_t)(buf + lq * (D * 2) + (((4 * db + g) ^ (lq & (kChunks - 1))) << 4) + 8 * half) = w;
+    }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const CtxRow mine = ctx_row(a, p, tile, kvh, row0 + lq);
+  const int64_t off = (int64_t)mine.head * a.o_head + (int64_t)mine.token * a.o_token;
+  uint16_t* const out = (uint16_t*)tab.out[tile];
+  const int sub = lane / kChunks, chunk = lane % kChunks;
+#pragma unroll
+  for (int i = 0; i < 32 / kRowsPer; ++i) {
+    const int r = kRowsPer * i + sub;
+    const int lo = __shfl((int)(uint32_t)off, r, 64), hi = __shfl((int)(off >> 32), r, 64);
+    const u32x4 x = *(const SG_LDS u32x4*)(uintptr_t)(buf + r * (D * 2) + ((chunk ^ (r & (kChunks - 1))) << 4));
+    if (row0 + r < p.rows) *(u32x4*)(out + ((int64_t)hi << 32 | (uint32_t)lo) + 8 * chunk) = x;
+  }
+}
+
+}  // namespace
+
+int launch_context_bf16(const CtxArgs& a, const CtxTable& tab, const CtxPlan& plan, int head_dim, hipStream_t s) {
+  int dev = 0;
+  SG_HIP_TRY(hipGetDevice(&dev));
+  // the kernels need more dynamic LDS than the default limit; the attribute is set once per device and kernel
+  constexpr int kMaxDevices = 64;
+  static std::atomic<bool> attr_set[kMaxDevices][4];
+  auto launch = [&](auto kern, int slot, int lds, int64_t grid) -> int {
+    if (grid > (1ll << 31) - 1) return SG_ERR_UNSUPPORTED;
+    if (grid == 0) return SG_OK;
+    if (dev < 0 || dev >= kMaxDevices || !attr_set[dev][slot].load(std::memory_order_acquire)) {
+      SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+      if (dev >= 0 && dev < kMaxDevices) attr_set[dev][slot].store(true, std::memory_order_release);
+    }
+    kern<<<dim3((unsigned)grid), 256, lds, s>>>(a, tab);
+    SG_HIP_TRY(hipGetLastError());
+    return SG_OK;
+  };
+  const int64_t grid = ((int64_t)a.part[0].items + 7) / 8 * 8 + ((int64_t)a.part[1].items + 7) / 8 * 8;
+  if (plan.wide)
+    return head_dim == 128 ? launch(context_bf16_wide_kernel<128>, 0, kWideLds<128>, grid) : launch(context_bf16_wide_kernel<64>, 1, kWideLds<64>, grid);
+  return head_dim == 128 ? launch(context_bf16_split_kernel<128>, 2, kSplitLds, grid) : launch(context_bf16_split_kernel<64>, 3, kSplitLds, grid);
+}
+
+}  // namespace sg

@@ -66,6 +66,8 @@ int launch_similarity(const void* const* x_new, const void* const* x_old, int n_
 int launch_region_thresholds(const float* tile_std, double* track_mean, int32_t* track_count, int n_tiles,
                              float tau_base, float alpha, int mode, int adjust, float* sigma, float* thresholds,
                              hipStream_t s);
+int launch_residual_norm(const sg_norm_problem& p, int n_tiles, const void* const* x, const void* const* residual, const void* weight,
+                         const uint8_t* run, void* const* sum, void* const* out, float* const* scale, hipStream_t s);
 int launch_cache_refresh(const void* const* src, void* const* dst, const uint8_t* recompute,
                          uint8_t* has_cache, int n_tiles, int64_t bytes_per_tile, hipStream_t s);
 
