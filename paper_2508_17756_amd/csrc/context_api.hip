@@ -95,7 +95,9 @@ static int attend(const sg_context_problem& p, bool prefix, int n_tiles, const v
     a.n_shares = plan.n_shares;
     a.scale = p.scale;
     a.part[0] = plan.part[0]; a.part[1] = plan.part[1];
-    int st = p.dtype == SG_F32 ? launch_context_f32(a, tab, plan, p.head_dim, s) : launch_context_bf16(a, tab, plan, p.head_dim, s);
+    int st = p.dtype == SG_F32 ? launch_context_f32(a, tab, plan, p.head_dim, s)
+             : plan.wide       ? launch_context_bf16_wide(a, tab, p.head_dim, s)
+                               : launch_context_bf16_split(a, tab, p.head_dim, s);
     if (st != SG_OK) return st;
     if (plan.n_shares > 1) {
       st = launch_context_join(a, tab, p.head_dim, p.dtype, s);

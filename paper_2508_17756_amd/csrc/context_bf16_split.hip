@@ -1,0 +1,225 @@
+// Context attention (sg_tile_cross_attention, sg_tile_prefix_attention) of calls with few rows, bf16: every wavefront streams keys of its own
+// through LDS of its own, 32 rows at a time, and the shares of a row are joined in LDS and, over workgroups, by the join kernel.
+#include <atomic>
+#include "context_bf16.h"
+
+namespace sg {
+namespace {
+
+// One row's softmax (the same in lanes l and l ^ 32) and its output accumulators.
+template <int D>
+struct RowState {
+  f32x16 o[D / 32];
+  float m;   // running maximum, log2 domain
+  float l;   // this lane's share of the sum
+};
+template <int D>
+__device__ __forceinline__ void clear(RowState<D>& st) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
+  st.m = -__builtin_inff();
+  st.l = 0.f;
+}
+
+// NB blocks of 32 keys, K at LDS address kb0 and V at vb0.  head_dim 128: block b is the slots 32 b .. 32 b + 31; head_dim 64: the 32 slots
+// hold two keys each and block b (of 2) is their b-th ones.
+template <int D, int NB>
+__device__ __forceinline__ void attend_keys(const Frags& f, const uint32_t kb0, const uint32_t vb0, const bf16x8 (&qf)[D / 16], const float c_log2,
+                                            const uint64_t valid, RowState<D>& st) {
+  static_assert(D == 128 || NB == 2, "");
+  constexpr uint64_t kFull = (D == 128 && NB == 1) ? 0xffffffffull : ~0ull;
+  f32x16 s[NB];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const uint32_t at = kb0 + f.k[D == 128 ? kk : 4 * b + kk] + (D == 128 ? b * 32 * kSlot : 0);
+      const bf16x8 x = __builtin_bit_cast(bf16x8, *(const SG_LDS u32x4*)(uintptr_t)at);
+      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[kk], kk == 0 ? zero16() : s[b], 0, 0, 0);
+    }
+  if (valid != kFull) mask_scores<D, NB>(s, valid);
+  float mx = s[0][0];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+  const uint32_t mu = __float_as_uint(mx);
+  const auto sw = __builtin_amdgcn_permlane32_swap(mu, mu, false, false);
+  mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  const float top = fmaxf(st.m, mx * c_log2);
+  if (__any(top != st.m)) {
+    const float alpha = st.m == top ? 1.f : __builtin_amdgcn_exp2f(st.m - top);   // first keys: exp2(-inf) = 0
+    st.m = top;
+    st.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) st.o[db] *= alpha;
+  }
+  const float ref = st.m == -__builtin_inff() ? 0.f : st.m;   // no key so far: probabilities 0
+  // The probabilities are rounded to bf16 for the second product (2^-9 of each, which averages out over a row); their sum is taken before.
+  float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 p;
+#pragma unroll
+      for (int r = 0; r < 8; r += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], c_log2, -ref));
+        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r + 1], c_log2, -ref));
+        sum0 += e0;
+        sum1 += e1;
+        p[r] = (__bf16)e0;
+        p[r + 1] = (__bf16)e1;
+      }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) {
+        const uint32_t at = vb0 + f.v[D == 128 ? db : 2 * b + db] + (D == 128 ? b * 32 * kSlot : 0) + h * 16 * kSlot;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)(at + 8 * kSlot));
+        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p, st.o[db], 0, 0, 0);
+      }
+    }
+  st.l += sum0 + sum1;
+}
+
+// ------------------------------------------------------------------------------------------------------ few rows
+// A wavefront's LDS: two stages of 32 slots of K and V.  After the keys it holds the wavefront's sums: 32 rows x D floats (16-byte chunk c of
+// row r at chunk c ^ r), then (reference, sum) of the rows.
+constexpr int kSplitStage = 2 * 32 * kSlot;              // 16 KiB
+constexpr int kSplitWave = 2 * kSplitStage;
+constexpr int kSplitLds = 4 * kSplitWave;
+constexpr int kSumsAt = kSplitStage;
+
+template <int D>
+__global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArgs a, const CtxTable tab) {
+  constexpr int kKeys = D == 128 ? 32 : 64, kBlocks = D == 128 ? 1 : 2;
+  constexpr uint64_t kFull = kKeys == 32 ? 0xffffffffull : ~0ull;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lq = lane & 31, half = lane >> 5;
+
+  const int grid0 = (a.part[0].items + 7) / 8 * 8;
+  const int which = (int)blockIdx.x < grid0 ? 0 : 1;
+  const CtxPart& p = a.part[which];
+  int id = ctx_xcd_order((int)blockIdx.x - (which ? grid0 : 0), p.items);
+  if (id < 0) return;
+  const int row_block = id % p.row_blocks;
+  id /= p.row_blocks;
+  const int split = id % p.splits;
+  id /= p.splits;
+  const int kvh = id % a.kv_heads, batch = id / a.kv_heads;
+  if (!p.stacked && a.run && a.run[batch] == 0) return;
+  const int way = wave & (p.ways - 1);
+  const int row0 = (row_block * (4 / p.ways) + wave / p.ways) * 32;
+
+  RowState<D> st;
+  clear(st);
+  if (row0 < p.rows) {
+    const Segment g0 = segment(a, tab, 0, batch, kvh), g1 = segment(a, tab, 1, batch, kvh);
+    const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
+    const int n = n0 + n1;
+    const int from = (int)((int64_t)n * split / p.splits), to = (int)((int64_t)n * (split + 1) / p.splits);
+    const uint32_t ring = lds0 + wave * kSplitWave;
+    uint64_t valid_next = 0;
+    auto issue = [&](int j, int at) SG_INLINE {
+      const bool second = j >= n0;
+      const Segment& g = second ? g1 : g0;
+      const int key0 = (second ? j - n0 : j) * kKeys;
+      bool counts = lane < kKeys && key0 + lane < g.len;
+      if (g.mask && counts) counts = g.mask[key0 + lane] != 0;
+      const uint64_t v = __ballot(counts);
+      valid_next = v;
+      const uint32_t dst = ring + at * kSplitStage;
+      move_half<D, 8>(g.k, g.token, key0, 0, v, false, dst, kFull);
+      move_half<D, 8>(g.v, g.token, key0, 0, v, true, dst + 32 * kSlot, kFull);
+    };
+    int j = from + way;
+    if (j < to) issue(j, 0);
+    bf16x8 qf[D / 16];
+    load_query<D>(a, tab, ctx_row(a, p, batch, kvh, row0 + lq), qf);
+    const Frags f = make_frags();
+    const float c_log2 = a.scale * 1.4426950408889634f;
+    for (int at = 0; j < to; j += p.ways, at ^= 1) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // this stage is there, the other one has been read
+      __builtin_amdgcn_sched_barrier(0);
+      const uint64_t v = valid_next;
+      if (j + p.ways < to) issue(j + p.ways, at ^ 1);
+      const uint32_t base = ring + at * kSplitStage;
+      if (v != 0) attend_keys<D, kBlocks>(f, base, base + 32 * kSlot, qf, c_log2, v, st);
+    }
+  }
+  const uint32_t lu = __float_as_uint(st.l);
+  const auto sw = __builtin_amdgcn_permlane32_swap(lu, lu, false, false);
+  const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+
+  // ---- join of the shares in this workgroup
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  const uint32_t mine = lds0 + wave * kSplitWave;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f32x4 x = {st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
+      *(SG_LDS f32x4*)(uintptr_t)(mine + lq * (D * 4) + (((8 * db + 2 * g + half) ^ (lq & (D / 4 - 1))) << 4)) = x;
+    }
+  if (half == 0) *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + lq * 8) = f32x2{st.m, l};
+  __syncthreads();
+  const uint32_t group = lds0 + (wave & ~(p.ways - 1)) * kSplitWave;
+  constexpr int kLanes = D / 4;   // lanes per row: 4 channels each
+  const int rows_at_once = 64 * p.ways / kLanes, tg = way * 64 + lane;
+  const int chunk = tg % kLanes;
+  for (int r = tg / kLanes; r < 32; r += rows_at_once) {
+    if (row0 + r >= p.rows) break;
+    const CtxRow row = ctx_row(a, p, batch, kvh, row0 + r);
+    if (!row.there) continue;
+    float top = -__builtin_inff();
+    for (int w = 0; w < p.ways; ++w) top = fmaxf(top, (*(const SG_LDS f32x2*)(uintptr_t)(group + w * kSplitWave + kSumsAt + r * 8))[0]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int w = 0; w < p.ways; ++w) {
+      const uint32_t at = group + w * kSplitWave;
+      const f32x2 ml = *(const SG_LDS f32x2*)(uintptr_t)(at + kSumsAt + r * 8);
+      if (ml[1] == 0.f) continue;   // a share without keys (one whose scores are NaN has a reference of -inf too)
+      const float e = __builtin_amdgcn_exp2f(ml[0] - top);
+      sum += e * ml[1];
+      acc += e * *(const SG_LDS f32x4*)(uintptr_t)(at + r * (D * 4) + ((chunk ^ (r & (D / 4 - 1))) << 4));
+    }
+    if (a.n_shares == 1) {
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+      uint16_t* const o = (uint16_t*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 4 * chunk;
+      *(u32x2*)o = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+    } else {
+      const int64_t at = (int64_t)row.rid * a.n_shares + p.first_share + split;
+      const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
+      *(f32x4*)(a.shares + at * D + 4 * chunk) = acc;
+      if (chunk == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{top, sum};
+    }
+  }
+}
+
+}  // namespace
+
+int launch_context_bf16_split(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s) {
+  int dev = 0;
+  SG_HIP_TRY(hipGetDevice(&dev));
+  // the kernels need more dynamic LDS than the default limit; the attribute is set once per device and kernel
+  constexpr int kMaxDevices = 64;
+  static std::atomic<bool> attr_set[kMaxDevices][2];
+  auto launch = [&](auto kern, int slot) -> int {
+    const int64_t grid = ((int64_t)a.part[0].items + 7) / 8 * 8 + ((int64_t)a.part[1].items + 7) / 8 * 8;
+    if (grid > (1ll << 31) - 1) return SG_ERR_UNSUPPORTED;
+    if (grid == 0) return SG_OK;
+    if (dev < 0 || dev >= kMaxDevices || !attr_set[dev][slot].load(std::memory_order_acquire)) {
+      SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kSplitLds));
+      if (dev >= 0 && dev < kMaxDevices) attr_set[dev][slot].store(true, std::memory_order_release);
+    }
+    kern<<<dim3((unsigned)grid), 256, kSplitLds, s>>>(a, tab);
+    SG_HIP_TRY(hipGetLastError());
+    return SG_OK;
+  };
+  return head_dim == 128 ? launch(context_bf16_split_kernel<128>, 0) : launch(context_bf16_split_kernel<64>, 1);
+}
+
+}  // namespace sg

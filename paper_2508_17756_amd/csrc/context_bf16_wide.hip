@@ -1,0 +1,301 @@
+// Context attention (sg_tile_cross_attention, sg_tile_prefix_attention) of calls with rows to fill the chip, bf16: products on the matrix
+// cores with fp32 accumulation, softmax in fp32, scores scaled in fp32 behind the product.
+//
+// A workgroup of 4 wavefronts takes 128 rows of one head of keys, 32 per wavefront, over both segments of keys in one pass; its wavefronts
+// share stages of 64 keys in LDS, two of keys and two of values.  The loop is pipelined inside a wavefront: iteration j takes the softmax
+// of stage j on the vector ALU between the products of its neighbours, PV of stage j - 1 and QK of stage j + 1, on the matrix pipe.  Two
+// workgroups run beside one another on a compute unit, so that the start and the end of one (rows in, rows out) hide behind the other.
+#include <atomic>
+#include <type_traits>
+#include "context_bf16.h"
+
+namespace sg {
+namespace {
+
+template <int D>
+constexpr int kWideSlots = D == 128 ? 64 : 32;
+template <int D>
+constexpr int kWideHalf = kWideSlots<D> * kSlot;   // keys (or values) of a stage
+template <int D>
+constexpr int kWideLds = 4 * kWideHalf<D>;         // two stages of keys, two of values
+
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+constexpr float kSlack = 5.f;   // log2: how far a score may pass the reference before the reference moves
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs a, const CtxTable tab) {
+  constexpr int kKeys = 64, kInstr = kWideSlots<D> / 16, kHalf = kWideHalf<D>;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lq = lane & 31, half = lane >> 5;
+  const CtxPart& p = a.part[0];
+  // Only the tiles that run are numbered, so that the work is spread evenly whichever they are.
+  uint64_t active = a.n_tiles >= 64 ? ~0ull : (1ull << a.n_tiles) - 1;
+  if (a.run) active = __ballot(lane < a.n_tiles && a.run[lane < a.n_tiles ? lane : 0] != 0);
+  const int per_tile = a.kv_heads * p.row_blocks;
+  const int id = ctx_xcd_order((int)blockIdx.x, __builtin_popcountll(active) * per_tile);
+  if (id < 0) return;
+  const int nth = id / per_tile, in_tile = id - nth * per_tile;
+  const int tile = __builtin_amdgcn_readfirstlane(ctx_nth_tile(active, nth));
+  const int kvh = __builtin_amdgcn_readfirstlane(in_tile / p.row_blocks), row_block = in_tile - kvh * p.row_blocks;
+  const int row0 = row_block * 128 + wave * 32;
+
+  const Segment g0 = segment(a, tab, 0, tile, kvh), g1 = segment(a, tab, 1, tile, kvh);
+  const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
+  const int n = n0 + n1;
+
+  bool mask_next = true;   // of the stage whose keys are requested next: whether key key0 + lane is unmasked
+  auto fetch_mask = [&](int j) SG_INLINE {
+    const int key = (j - n0) * kKeys + lane;
+    mask_next = !(j >= n0 && j < n && g1.mask) || (key < g1.len && g1.mask[key] != 0);
+  };
+  const int first = wave * (kWideSlots<D> / 4);
+  auto request = [&](int j, uint64_t v, bool is_v) SG_INLINE {
+    const bool second = j >= n0;
+    const Segment& g = second ? g1 : g0;
+    const int key0 = (second ? j - n0 : j) * kKeys;
+    const uint32_t dst = lds0 + (is_v ? 2 * kHalf : 0) + (j & 1) * kHalf + first * kSlot;
+    move_half<D, kInstr>(is_v ? g.v : g.k, g.token, key0, first, v, is_v, dst);
+  };
+  // which of its keys count
+  auto counting = [&](int j) SG_INLINE -> uint64_t {
+    const bool second = j >= n0;
+    const int key0 = (second ? j - n0 : j) * kKeys;
+    const uint64_t v = __ballot(mask_next && key0 + lane < (second ? g1.len : g0.len));
+    if (g1.mask) fetch_mask(j + 1);
+    return v;
+  };
+  uint64_t v_now = 0, v_next = 0, v_later = 0;   // of the stages j, j + 1, j + 2
+  if (n > 0) {
+    if (g1.mask) fetch_mask(0);
+    v_now = counting(0);
+    request(0, v_now, false);
+  }
+  bf16x8 qf[D / 16];
+  load_query<D>(a, tab, ctx_row(a, p, tile, kvh, row0 + lq), qf);
+  Frags f = make_frags();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f.k[i] += lds0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f.v[i] += lds0;
+  int side = kHalf;
+  auto turn = [&]() SG_INLINE {   // fragments are read from the other one of the two stages
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.k[i] += side;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] += side;
+    side = -side;
+  };
+  const float c_log2 = a.scale * 1.4426950408889634f;
+  f32x16 o[D / 32], s[2];
+  bf16x8 pr[4];
+  float m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) o[db] = zero16();
+
+  auto meet = [&]() SG_INLINE {   // own transfers have landed; behind the barrier everyone's, and nobody reads what is requested next
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // Fragment reads run kAhead steps (matrix instructions) ahead of their use; the scheduling barriers keep the compiler from gathering
+  // them behind one another.
+  constexpr int kAhead = 2, kDb = D / 32, kPv = 4 * kDb, kQk = 2 * (D / 16);
+  auto kfrag = [&](uint32_t at0, int u) SG_INLINE -> bf16x8 {   // step u: block u / (D / 16), channels 16 (u % (D / 16)) .. + 15
+    const int kk = u % (D / 16), b = u / (D / 16);
+    const uint32_t at = at0 + f.k[D == 128 ? kk : 4 * b + kk] + (D == 128 ? b * 32 * kSlot : 0);
+    return __builtin_bit_cast(bf16x8, *(const SG_LDS u32x4*)(uintptr_t)at);
+  };
+  auto vfrag = [&](uint32_t at0, int t) SG_INLINE -> bf16x8 {   // step t: the 16 keys of pr[t / kDb], channels 32 (t % kDb) .. + 31
+    const int i = t / kDb, db = t % kDb, b = i >> 1, h = i & 1;
+    const uint32_t at = at0 + f.v[D == 128 ? db : 2 * b + db] + (D == 128 ? b * 32 * kSlot : 0) + h * 16 * kSlot;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)(at + 8 * kSlot));
+    const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, both);
+  };
+  bf16x8 ka[kQk], va[kPv];
+  float alpha = 1.f, neg = 0.f, sum0 = 0.f, sum1 = 0.f;
+  bool rescale = false;
+  // Step t of a stage's softmax: the reference first, then a share of the exponentials, each rounded into pr when the product before has used
+  // what was there.
+  auto softmax_step = [&](int t) SG_INLINE {
+    if (t == 0) {
+      float mx0 = s[0][0], mx1 = s[1][0];
+#pragma unroll
+      for (int r = 1; r < 15; r += 2) {
+        mx0 = fmaxf(fmaxf(mx0, s[0][r]), s[0][r + 1]);
+        mx1 = fmaxf(fmaxf(mx1, s[1][r]), s[1][r + 1]);
+      }
+      float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(s[0][15], s[1][15]));
+      const uint32_t mu = __float_as_uint(mx);
+      const auto sw = __builtin_amdgcn_permlane32_swap(mu, mu, false, false);
+      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c_log2;
+      const float moved = mx > m + kSlack ? mx : m;
+      rescale = __any(moved != m);
+      alpha = __builtin_amdgcn_exp2f(moved == m ? 0.f : m - moved);   // first keys: exp2(-inf) = 0
+      m = moved;
+      neg = m == -__builtin_inff() ? 0.f : -m;   // no key so far: probabilities 0
+      sum0 = sum1 = 0.f;
+    }
+    constexpr int kSteps = kPv + kQk / 2 - 1;
+    const int lo = t == 0 ? 0 : (t - 1) * 32 / kSteps, hi = t * 32 / kSteps;
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e >= lo && e < hi) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 4][e & 15], c_log2, neg));
+        s[e >> 4][e & 15] = x;
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (8 * i + 8 > lo && 8 * i + 8 <= hi) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) pr[i][r] = (__bf16)s[i >> 1][8 * (i & 1) + r];
+        asm volatile("" : "+v"(pr[i]));
+        const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+        for (int r = 0; r < 8; r += 2) {
+          const bf16x2 two = {pr[i][r], pr[i][r + 1]};
+          if (r & 2) sum1 = __builtin_amdgcn_fdot2_f32_bf16(two, ones, sum1, false);
+          else sum0 = __builtin_amdgcn_fdot2_f32_bf16(two, ones, sum0, false);
+        }
+      }
+  };
+  auto qk = [&](uint32_t at0, bool begun, bool soft) SG_INLINE {
+    if (!begun) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) ka[u] = kfrag(at0, u);
+    }
+#pragma unroll
+    for (int u = 0; u < kQk; ++u) {
+      if (u + kAhead < kQk) ka[u + kAhead] = kfrag(at0, u + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+      const int b = u / (D / 16), kk = u % (D / 16);
+      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[u], qf[kk], kk == 0 ? zero16() : s[b], 0, 0, 0);
+      if (soft && b == 0) softmax_step(kPv + u);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto iteration = [&](int j, auto has_before, auto has_after) SG_INLINE {
+    constexpr bool BEFORE = decltype(has_before)::value, AFTER = decltype(has_after)::value;
+    meet();
+    if (AFTER && j + 2 < n) {
+      v_later = counting(j + 2);
+      request(j + 2, v_later, false);
+    }
+    request(j, v_now, true);
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr uint32_t k_at = 0, v_at = 2 * kHalf;   // of the other stage (the addresses change sides)
+    turn();
+    if (BEFORE) {
+#pragma unroll
+      for (int t = 0; t < kAhead; ++t) va[t] = vfrag(v_at, t);
+    }
+#pragma unroll
+    for (int t = 0; t < kPv; ++t) {
+      if (BEFORE && t + kAhead < kPv) va[t + kAhead] = vfrag(v_at, t + kAhead);
+      else if (AFTER && t + kAhead >= kPv) ka[t + kAhead - kPv] = kfrag(k_at, t + kAhead - kPv);
+      __builtin_amdgcn_sched_barrier(0);
+      if (BEFORE) o[t % kDb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[t], pr[t / kDb], o[t % kDb], 0, 0, 0);
+      softmax_step(t);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (AFTER) {
+      qk(k_at, true, true);
+    } else {
+#pragma unroll
+      for (int t = kPv; t < kPv + kQk / 2; ++t) softmax_step(t);
+    }
+    l = l * alpha + (sum0 + sum1);
+    if (rescale) {
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) o[db] *= alpha;
+    }
+    if (AFTER && v_next != ~0ull) mask_scores<D, 2>(s, v_next);
+    v_now = v_next;
+    v_next = v_later;
+  };
+  if (n > 0) {
+    meet();
+    if (n > 1) {
+      v_next = counting(1);
+      request(1, v_next, false);
+    }
+    qk(0, false, false);
+    if (v_now != ~0ull) mask_scores<D, 2>(s, v_now);
+    using T = std::true_type;
+    using F = std::false_type;
+    if (n == 1) iteration(0, F{}, F{});
+    else {
+      iteration(0, F{}, T{});
+      for (int j = 1; j < n - 1; ++j) iteration(j, T{}, T{});
+      iteration(n - 1, T{}, F{});
+    }
+    meet();
+    constexpr uint32_t v_at = 2 * kHalf;
+    turn();
+#pragma unroll
+    for (int t = 0; t < kAhead; ++t) va[t] = vfrag(v_at, t);
+#pragma unroll
+    for (int t = 0; t < kPv; ++t) {
+      if (t + kAhead < kPv) va[t + kAhead] = vfrag(v_at, t + kAhead);
+      __builtin_amdgcn_sched_barrier(0);
+      o[t % kDb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[t], pr[t / kDb], o[t % kDb], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  // ---- rows go out through LDS (8 KiB a wavefront), so that a store writes whole rows; chunk c of row r sits at chunk c ^ (r % kChunks)
+  constexpr int kChunks = D / 8, kRowsPer = 64 / kChunks;
+  const uint32_t lu = __float_as_uint(l);
+  const auto sw = __builtin_amdgcn_permlane32_swap(lu, lu, false, false);
+  l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  static_assert(4 * 32 * D * 2 <= 2 * kHalf, "rows go through the keys' half of LDS, which nobody reads after the last barrier");
+  const uint32_t buf = lds0 + wave * (32 * D * 2);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const u32x2 w = {pack_bf16x2(o[db][4 * g] * inv, o[db][4 * g + 1] * inv), pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv)};
+      *(SG_LDS u32x2*)(uintptr_t)(buf + lq * (D * 2) + (((4 * db + g) ^ (lq & (kChunks - 1))) << 4) + 8 * half) = w;
+    }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  const CtxRow mine = ctx_row(a, p, tile, kvh, row0 + lq);
+  const int64_t off = (int64_t)mine.head * a.o_head + (int64_t)mine.token * a.o_token;
+  uint16_t* const out = (uint16_t*)tab.out[tile];
+  const int sub = lane / kChunks, chunk = lane % kChunks;
+#pragma unroll
+  for (int i = 0; i < 32 / kRowsPer; ++i) {
+    const int r = kRowsPer * i + sub;
+    const int lo = __shfl((int)(uint32_t)off, r, 64), hi = __shfl((int)(off >> 32), r, 64);
+    const u32x4 x = *(const SG_LDS u32x4*)(uintptr_t)(buf + r * (D * 2) + ((chunk ^ (r & (kChunks - 1))) << 4));
+    if (row0 + r < p.rows) *(u32x4*)(out + ((int64_t)hi << 32 | (uint32_t)lo) + 8 * chunk) = x;
+  }
+}
+
+}  // namespace
+
+int launch_context_bf16_wide(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s) {
+  int dev = 0;
+  SG_HIP_TRY(hipGetDevice(&dev));
+  constexpr int kMaxDevices = 64;
+  static std::atomic<bool> attr_set[kMaxDevices][2];   // the kernels' dynamic-LDS limit has been raised
+  auto launch = [&](auto kern, int slot, int lds) -> int {
+    const int64_t grid = ((int64_t)a.part[0].items + 7) / 8 * 8;
+    if (grid == 0) return SG_OK;
+    if (dev < 0 || dev >= kMaxDevices || !attr_set[dev][slot].load(std::memory_order_acquire)) {
+      SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+      if (dev >= 0 && dev < kMaxDevices) attr_set[dev][slot].store(true, std::memory_order_release);
+    }
+    kern<<<dim3((unsigned)grid), 256, lds, s>>>(a, tab);
+    SG_HIP_TRY(hipGetLastError());
+    return SG_OK;
+  };
+  return head_dim == 128 ? launch(context_bf16_wide_kernel<128>, 0, kWideLds<128>) : launch(context_bf16_wide_kernel<64>, 1, kWideLds<64>);
+}
+
+}  // namespace sg

@@ -96,14 +96,15 @@ __device__ __forceinline__ CtxRow ctx_row(const CtxArgs& a, const CtxPart& p, in
 // ---------------------------------------------------------------------------------------------------- host side
 // The launches of one call (at most kCtxTilesPerLaunch tiles each) and what they need of the workspace.
 struct CtxPlan {
-  bool wide;             // bf16: workgroups of 128 rows share their keys in LDS, nothing is split
+  bool wide;             // workgroups of 128 rows share their keys in LDS, nothing is split
   int32_t wave_rows;     // otherwise rows of a wavefront: 32 (fp32: or 16)
   int32_t n_shares;
   CtxPart part[2];
   size_t bytes;          // workspace
 };
 CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles);
-int launch_context_bf16(const CtxArgs& a, const CtxTable& tab, const CtxPlan& plan, int head_dim, hipStream_t s);
+int launch_context_bf16_wide(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s);
+int launch_context_bf16_split(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s);
 int launch_context_f32(const CtxArgs& a, const CtxTable& tab, const CtxPlan& plan, int head_dim, hipStream_t s);
 int launch_context_join(const CtxArgs& a, const CtxTable& tab, int head_dim, int dtype, hipStream_t s);
 

@@ -4,8 +4,12 @@
 // S^T = K Q^T puts one row (query) per lane column and four keys in a lane's registers, which are then the B operands of
 // O^T = V^T P^T as they stand: step r of a block of 16 keys contracts the keys 4 g + r of the four lane groups g.
 //
-// Every wavefront streams keys of its own through LDS of its own, against 16 QB rows; wavefronts of a workgroup take other row blocks or other
-// shares of the keys, whichever there are more of (context_common.h).  Bound by the matrix instruction from 8 or so rows on, below by memory.
+// Row i of block db of O^T is channel 64 (db / 4) + 4 i + db % 4, so that a lane reads its values of four blocks, and writes its results, 16
+// bytes at a time.
+//
+// Two forms.  Shared: the 4 wavefronts of a workgroup take rows of their own against the same stages of keys, for calls with rows to fill the
+// chip.  Otherwise every wavefront streams keys of its own through LDS of its own; wavefronts of a workgroup take other row blocks or other
+// shares of the keys, whichever there are more of (context_common.h).
 #include <atomic>
 #include "context_common.h"
 
@@ -39,13 +43,27 @@ __device__ __forceinline__ Segment segment(const CtxArgs& a, const CtxTable& tab
   return g;
 }
 
-template <int D, int QB>
-__global__ __launch_bounds__(256, 1) void context_f32_kernel(const CtxArgs a, const CtxTable tab) {
+// max / sum over the four lane groups
+__device__ __forceinline__ float group_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float group_sum(float x) {
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+
+template <int D, int QB, bool SHARED>
+__global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const CtxArgs a, const CtxTable tab) {
   constexpr int kKeys = kHalfStage / (D * 4);   // 16 (head_dim 64: 32)
   constexpr int kBlocks = kKeys / 16;
   constexpr int kChunks = D / 4;                // 16-byte chunks of a row
   constexpr int kRowsPer = 64 / kChunks;        // rows one transfer moves
   constexpr int kRows = 16 * QB;
+  constexpr int kTransfers = SHARED ? 2 : 8;    // of a wavefront, of keys and as many of values
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -64,7 +82,7 @@ __global__ __launch_bounds__(256, 1) void context_f32_kernel(const CtxArgs a, co
   if (!p.stacked && a.run && a.run[batch] == 0) return;
   const int way = wave & (p.ways - 1);
   const int row0 = (row_block * (4 / p.ways) + wave / p.ways) * kRows;
-  const uint32_t mine = lds0 + wave * kWaveLds;
+  const uint32_t mine = SHARED ? lds0 : lds0 + wave * kWaveLds;
 
   f32x4 o[QB][D / 16];
   float m[QB], l[QB];
@@ -75,15 +93,15 @@ __global__ __launch_bounds__(256, 1) void context_f32_kernel(const CtxArgs a, co
     m[qb] = -__builtin_inff();
     l[qb] = 0.f;
   }
-  if (row0 < p.rows) {
+  if (SHARED || row0 < p.rows) {
     const Segment g0 = segment(a, tab, 0, batch, kvh), g1 = segment(a, tab, 1, batch, kvh);
     const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
     const int n = n0 + n1;
     const int from = (int)((int64_t)n * split / p.splits), to = (int)((int64_t)n * (split + 1) / p.splits);
     constexpr uint32_t kFull = kKeys == 32 ? 0xffffffffu : 0xffffu;
     uint32_t valid_next = 0;
-    // 16-byte chunk c of K row r sits at chunk c ^ (r & 15), of V row r at c ^ (((r >> 2) & 3) << 2): the rows that one fragment read
-    // touches then lie on different banks
+    // 16-byte chunk c of K row r sits at chunk c ^ (r & 15), so that the 16 rows that a fragment read touches lie on different banks; V rows
+    // are read along and stay as they are
     auto issue = [&](int j, int at) SG_INLINE {
       const bool second = j >= n0;
       const Segment& g = second ? g1 : g0;
@@ -92,26 +110,26 @@ __global__ __launch_bounds__(256, 1) void context_f32_kernel(const CtxArgs a, co
       if (g.mask && counts) counts = g.mask[key0 + lane] != 0;
       const uint32_t valid = (uint32_t)__ballot(counts);
       valid_next = valid;
-      const uint32_t dst = mine + at * kStage;
+      const int first = SHARED ? wave * kTransfers : 0;
+      const uint32_t dst = mine + at * kStage + first * 1024;
       const char* const kp = g.k + (int64_t)key0 * g.token;
       const char* const vp = g.v + (int64_t)key0 * g.token;
       const int sub = lane / kChunks, c = lane % kChunks;
       if (valid == kFull) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int r = kRowsPer * u + sub;
+        for (int u = 0; u < kTransfers; ++u) {
+          const int r = kRowsPer * (first + u) + sub;
           dma16(kp, (uint32_t)r * g.token + (uint32_t)((c ^ (r & 15)) << 4), dst + u * 1024);
-          dma16(vp, (uint32_t)r * g.token + (uint32_t)((c ^ (((r >> 2) & 3) << 2)) << 4), dst + kHalfStage + u * 1024);
+          dma16(vp, (uint32_t)r * g.token + (uint32_t)(c << 4), dst + kHalfStage + u * 1024);
         }
       } else {   // keys that do not count are read from the zeros
-        const char* const zeros = (const char*)g_ctx_zeros;
+        const char* const zeros = (const char*)g_ctx_zeros + ((c & 15) << 4);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int r = kRowsPer * u + sub;
+        for (int u = 0; u < kTransfers; ++u) {
+          const int r = kRowsPer * (first + u) + sub;
           const bool on = (valid >> r) & 1;
-          dma16_addr(on ? kp + ((uint32_t)r * g.token + (uint32_t)((c ^ (r & 15)) << 4)) : zeros + ((c & 15) << 4), dst + u * 1024);
-          dma16_addr(on ? vp + ((uint32_t)r * g.token + (uint32_t)((c ^ (((r >> 2) & 3) << 2)) << 4)) : zeros + ((c & 15) << 4),
-                     dst + kHalfStage + u * 1024);
+          dma16_addr(on ? kp + ((uint32_t)r * g.token + (uint32_t)((c ^ (r & 15)) << 4)) : zeros, dst + u * 1024);
+          dma16_addr(on ? vp + ((uint32_t)r * g.token + (uint32_t)(c << 4)) : zeros, dst + kHalfStage + u * 1024);
         }
       }
     };
@@ -129,35 +147,53 @@ __global__ __launch_bounds__(256, 1) void context_f32_kernel(const CtxArgs a, co
         q[qb][jj] = row.there ? x * a.scale : f32x4{0.f, 0.f, 0.f, 0.f};
       }
     }
-    uint32_t kfrag[D / 16], vfrag[D / 16];   // offsets inside a half stage: rows lq; rows 4 grp (+ r), channel lq of block db
+    uint32_t kfrag[D / 16];   // offsets inside a half stage: row lq, chunk 4 jj + grp
 #pragma unroll
-    for (int jj = 0; jj < D / 16; ++jj) {
-      kfrag[jj] = lq * (D * 4) + (((4 * jj + grp) ^ lq) << 4);
-      vfrag[jj] = kHalfStage + 4 * grp * (D * 4) + (((4 * jj + (lq >> 2)) ^ (grp << 2)) << 4) + (lq & 3) * 4;
-    }
+    for (int jj = 0; jj < D / 16; ++jj) kfrag[jj] = lq * (D * 4) + (((4 * jj + grp) ^ lq) << 4);
+    const uint32_t vfrag = kHalfStage + 4 * grp * (D * 4) + lq * 16;   // rows 4 grp (+ r), channels 4 lq (+ 64)
     for (int at = 0; j < to; j += p.ways, at ^= 1) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // this stage is there, the other one has been read
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (SHARED) {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      }
       const uint32_t valid = valid_next;
       if (j + p.ways < to) issue(j + p.ways, at ^ 1);
       if (valid == 0) continue;
       const uint32_t base = mine + at * kStage;
+      // Fragments are read a group of matrix instructions ahead: those of K before the first product, those of V before the softmax.
+      f32x4 kf[kBlocks][D / 16], vf[kBlocks][4][D / 64];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int jj = 0; jj < D / 16; ++jj) kf[b][jj] = *(const SG_LDS f32x4*)(uintptr_t)(base + kfrag[jj] + b * 16 * D * 4);
+      __builtin_amdgcn_sched_barrier(0);
       f32x4 s[QB][kBlocks];
 #pragma unroll
-      for (int b = 0; b < kBlocks; ++b) {
+      for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) s[qb][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int jj = 0; jj < D / 16; ++jj) {
-          const f32x4 x = *(const SG_LDS f32x4*)(uintptr_t)(base + kfrag[jj] + b * 16 * D * 4);
+      for (int jj = 0; jj < D / 16; ++jj)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) s[qb][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], q[qb][jj][e], s[qb][b], 0, 0, 0);
-        }
-      }
-      if (valid != kFull) {
-        const uint32_t own_keys = valid >> (4 * grp);
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) s[qb][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][jj][e], q[qb][jj][e], s[qb][b], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int h = 0; h < D / 64; ++h) vf[b][r][h] = *(const SG_LDS f32x4*)(uintptr_t)(base + vfrag + (16 * b + r) * (D * 4) + h * 256);
+      __builtin_amdgcn_sched_barrier(0);
+      if (__builtin_expect(valid != kFull, 0)) {
+        uint32_t own_keys = valid >> (4 * grp);
+        asm volatile("" : "+v"(own_keys));
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -173,8 +209,7 @@ __global__ __launch_bounds__(256, 1) void context_f32_kernel(const CtxArgs a, co
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
           for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[qb][b][r]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = group_max(mx);
         const float top = fmaxf(m[qb], mx);
         if (__any(top != m[qb])) {
           const float alpha = m[qb] == top ? 1.f : __builtin_amdgcn_exp2f((m[qb] - top) * kLog2e);   // first keys: exp2(-inf) = 0
@@ -197,52 +232,71 @@ __global__ __launch_bounds__(256, 1) void context_f32_kernel(const CtxArgs a, co
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int db = 0; db < D / 16; ++db) {
-            const float x = *(const SG_LDS float*)(uintptr_t)(base + vfrag[db] + (16 * b + r) * D * 4);
+          for (int db = 0; db < D / 16; ++db)
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) o[qb][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s[qb][b][r], o[qb][db], 0, 0, 0);
-          }
+            for (int qb = 0; qb < QB; ++qb)
+              o[qb][db] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[b][r][db >> 2][db & 3], s[qb][b][r], o[qb][db], 0, 0, 0);
     }
   }
-  // ---- join of the shares in this workgroup; chunk c of row r at chunk c ^ (r & 15)
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    l[qb] += __shfl_xor(l[qb], 16, 64);
-    l[qb] += __shfl_xor(l[qb], 32, 64);
+  for (int qb = 0; qb < QB; ++qb) l[qb] = group_sum(l[qb]);
+  // a lane's results: channels 64 h + 16 grp + 4 r .. + 3 of its query
+  auto four = [&](int qb, int h, int r) SG_INLINE -> f32x4 {
+    return f32x4{o[qb][4 * h][r], o[qb][4 * h + 1][r], o[qb][4 * h + 2][r], o[qb][4 * h + 3][r]};
+  };
+  if constexpr (SHARED) {
 #pragma unroll
-    for (int db = 0; db < D / 16; ++db)
-      *(SG_LDS f32x4*)(uintptr_t)(mine + (16 * qb + lq) * (D * 4) + (((4 * db + grp) ^ lq) << 4)) = o[qb][db];
-    if (grp == 0) *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + (16 * qb + lq) * 8) = f32x2{m[qb], l[qb]};
-  }
-  __syncthreads();
-  const uint32_t group = lds0 + (wave & ~(p.ways - 1)) * kWaveLds;
-  const int rows_at_once = 64 * p.ways / kChunks, tg = way * 64 + lane;
-  const int chunk = tg % kChunks;
-  for (int r = tg / kChunks; r < kRows; r += rows_at_once) {
-    if (row0 + r >= p.rows) break;
-    const CtxRow row = ctx_row(a, p, batch, kvh, row0 + r);
-    if (!row.there) continue;
-    float top = -__builtin_inff();
-    for (int w = 0; w < p.ways; ++w) top = fmaxf(top, (*(const SG_LDS f32x2*)(uintptr_t)(group + w * kWaveLds + kSumsAt + r * 8))[0]);
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int w = 0; w < p.ways; ++w) {
-      const uint32_t at = group + w * kWaveLds;
-      const f32x2 ml = *(const SG_LDS f32x2*)(uintptr_t)(at + kSumsAt + r * 8);
-      if (ml[1] == 0.f) continue;   // a share without keys (one whose scores are NaN has a reference of -inf too)
-      const float e = __builtin_amdgcn_exp2f((ml[0] - top) * kLog2e);
-      sum += e * ml[1];
-      acc += e * *(const SG_LDS f32x4*)(uintptr_t)(at + r * (D * 4) + ((chunk ^ (r & 15)) << 4));
+    for (int qb = 0; qb < QB; ++qb) {
+      if (row0 + 16 * qb + lq >= p.rows) continue;
+      const CtxRow row = ctx_row(a, p, batch, kvh, row0 + 16 * qb + lq);
+      float* const dst = (float*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 16 * grp;
+      const float inv = l[qb] == 0.f ? 0.f : 1.f / l[qb];
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) *(f32x4*)(dst + 64 * h + 4 * r) = four(qb, h, r) * inv;
     }
-    if (a.n_shares == 1) {
-      float* const dst = (float*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 4 * chunk;
-      *(f32x4*)dst = sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc / sum;
-    } else {
-      const int64_t at = (int64_t)row.rid * a.n_shares + p.first_share + split;
-      const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
-      *(f32x4*)(a.shares + at * D + 4 * chunk) = acc;
-      if (chunk == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{top * kLog2e, sum};
+  } else {
+    // ---- join of the shares in this workgroup; chunk c of row r at chunk c ^ (r & 15)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *(SG_LDS f32x4*)(uintptr_t)(mine + (16 * qb + lq) * (D * 4) + (((16 * h + 4 * grp + r) ^ lq) << 4)) = four(qb, h, r);
+      if (grp == 0) *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + (16 * qb + lq) * 8) = f32x2{m[qb], l[qb]};
+    }
+    __syncthreads();
+    const uint32_t group = lds0 + (wave & ~(p.ways - 1)) * kWaveLds;
+    const int rows_at_once = 64 * p.ways / kChunks, tg = way * 64 + lane;
+    const int chunk = tg % kChunks;
+    for (int r = tg / kChunks; r < kRows; r += rows_at_once) {
+      if (row0 + r >= p.rows) break;
+      const CtxRow row = ctx_row(a, p, batch, kvh, row0 + r);
+      if (!row.there) continue;
+      float top = -__builtin_inff();
+      for (int w = 0; w < p.ways; ++w) top = fmaxf(top, (*(const SG_LDS f32x2*)(uintptr_t)(group + w * kWaveLds + kSumsAt + r * 8))[0]);
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      float sum = 0.f;
+      for (int w = 0; w < p.ways; ++w) {
+        const uint32_t at = group + w * kWaveLds;
+        const f32x2 ml = *(const SG_LDS f32x2*)(uintptr_t)(at + kSumsAt + r * 8);
+        if (ml[1] == 0.f) continue;   // a share without keys (one whose scores are NaN has a reference of -inf too)
+        const float e = __builtin_amdgcn_exp2f((ml[0] - top) * kLog2e);
+        sum += e * ml[1];
+        acc += e * *(const SG_LDS f32x4*)(uintptr_t)(at + r * (D * 4) + ((chunk ^ (r & 15)) << 4));
+      }
+      if (a.n_shares == 1) {
+        float* const dst = (float*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 4 * chunk;
+        *(f32x4*)dst = sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc / sum;
+      } else {
+        const int64_t at = (int64_t)row.rid * a.n_shares + p.first_share + split;
+        const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
+        *(f32x4*)(a.shares + at * D + 4 * chunk) = acc;
+        if (chunk == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{top * kLog2e, sum};
+      }
     }
   }
 }
@@ -253,22 +307,24 @@ int launch_context_f32(const CtxArgs& a, const CtxTable& tab, const CtxPlan& pla
   int dev = 0;
   SG_HIP_TRY(hipGetDevice(&dev));
   constexpr int kMaxDevices = 64;
-  static std::atomic<bool> attr_set[kMaxDevices][4];   // the kernels' dynamic-LDS limit has been raised
-  auto launch = [&](auto kern, int slot) -> int {
+  static std::atomic<bool> attr_set[kMaxDevices][6];   // the kernels' dynamic-LDS limit has been raised
+  auto launch = [&](auto kern, int slot, int lds) -> int {
     const int64_t grid = ((int64_t)a.part[0].items + 7) / 8 * 8 + ((int64_t)a.part[1].items + 7) / 8 * 8;
     if (grid > (1ll << 31) - 1) return SG_ERR_UNSUPPORTED;
     if (grid == 0) return SG_OK;
     if (dev < 0 || dev >= kMaxDevices || !attr_set[dev][slot].load(std::memory_order_acquire)) {
-      SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kLds));
+      SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
       if (dev >= 0 && dev < kMaxDevices) attr_set[dev][slot].store(true, std::memory_order_release);
     }
-    kern<<<dim3((unsigned)grid), 256, kLds, s>>>(a, tab);
+    kern<<<dim3((unsigned)grid), 256, lds, s>>>(a, tab);
     SG_HIP_TRY(hipGetLastError());
     return SG_OK;
   };
+  if (plan.wide)
+    return head_dim == 128 ? launch(context_f32_kernel<128, 2, true>, 4, kWaveLds) : launch(context_f32_kernel<64, 2, true>, 5, kWaveLds);
   if (plan.wave_rows == 16)
-    return head_dim == 128 ? launch(context_f32_kernel<128, 1>, 0) : launch(context_f32_kernel<64, 1>, 1);
-  return head_dim == 128 ? launch(context_f32_kernel<128, 2>, 2) : launch(context_f32_kernel<64, 2>, 3);
+    return head_dim == 128 ? launch(context_f32_kernel<128, 1, false>, 0, kLds) : launch(context_f32_kernel<64, 1, false>, 1, kLds);
+  return head_dim == 128 ? launch(context_f32_kernel<128, 2, false>, 2, kLds) : launch(context_f32_kernel<64, 2, false>, 3, kLds);
 }
 
 }  // namespace sg

@@ -69,7 +69,7 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
   plan.part[0].seg0 = prefix;
   plan.part[0].seg1 = 1;
   const int64_t wide_blocks = (rows + 127) / 128, wide_items = (int64_t)n_tiles * p.kv_heads * wide_blocks;
-  if (bf16 && wide_items >= 256) {
+  if (wide_items >= 256) {
     plan.wide = true;
     plan.wave_rows = 32;
     plan.part[0].items = wide_items > (1 << 30) ? -1 : (int32_t)wide_items;
