@@ -31,7 +31,7 @@ static int validate(const sg_context_problem* p) {
   // offsets inside a stage of 64 keys are 32-bit; rows and items are numbered in 32 bits, for 64 tiles a launch
   if ((p->ctx_tokens > 0 && p->ctx_stride_token >= (1ll << 22)) || (p->own_tokens > 0 && p->own_stride_token >= (1ll << 22)))
     return SG_ERR_UNSUPPORTED;
-  if ((int64_t)p->heads * p->tokens >= (1ll << 25)) return SG_ERR_UNSUPPORTED;
+  if ((int64_t)p->heads * p->tokens >= (1ll << 25) || p->kv_heads > 65535) return SG_ERR_UNSUPPORTED;
   if (p->ctx_tokens >= (1 << 30) || p->own_tokens >= (1 << 30)) return SG_ERR_UNSUPPORTED;
   return SG_OK;
 }
@@ -64,12 +64,16 @@ static int attend(const sg_context_problem& p, bool prefix, int n_tiles, const v
   if (check_tiles(q, n_tiles) != SG_OK || check_tiles((const void* const*)out, n_tiles) != SG_OK) return SG_ERR_INVALID_ARG;
   if (tile_keys > 0 && (check_tiles(k, n_tiles) != SG_OK || check_tiles(v, n_tiles) != SG_OK)) return SG_ERR_INVALID_ARG;
   if (prefix && p.ctx_tokens > 0 && (!pk || !pv || !aligned16(pk) || !aligned16(pv))) return SG_ERR_INVALID_ARG;
+  for (int n : {n_tiles < kCtxTilesPerLaunch ? n_tiles : kCtxTilesPerLaunch, n_tiles % kCtxTilesPerLaunch}) {
+    if (n == 0) continue;
+    const CtxPlan plan = plan_context(p, prefix, n);
+    if (plan.part[0].items < 0 || plan.part[1].items < 0) return SG_ERR_UNSUPPORTED;
+  }
   const size_t need = workspace_bytes(p, prefix, n_tiles);
   if (need > 0 && (!ws || (((uintptr_t)ws) & 255u) || ws_bytes < need)) return SG_ERR_WORKSPACE;
   for (int t0 = 0; t0 < n_tiles; t0 += kCtxTilesPerLaunch) {
     const int n = n_tiles - t0 < kCtxTilesPerLaunch ? n_tiles - t0 : kCtxTilesPerLaunch;
     const CtxPlan plan = plan_context(p, prefix, n);
-    if (plan.part[0].items < 0 || plan.part[1].items < 0) return SG_ERR_UNSUPPORTED;
     CtxTable tab = {};
     for (int i = 0; i < n; ++i) {
       tab.q[i] = q[t0 + i];
@@ -94,13 +98,15 @@ static int attend(const sg_context_problem& p, bool prefix, int n_tiles, const v
     a.heads = p.heads; a.kv_heads = p.kv_heads; a.group = p.heads / p.kv_heads; a.tokens = p.tokens; a.n_tiles = n;
     a.n_shares = plan.n_shares;
     a.scale = p.scale;
-    a.part[0] = plan.part[0]; a.part[1] = plan.part[1];
-    int st = p.dtype == SG_F32 ? launch_context_f32(a, tab, plan, p.head_dim, s)
-             : plan.wide       ? launch_context_bf16_wide(a, tab, p.head_dim, s)
-                               : launch_context_bf16_split(a, tab, p.head_dim, s);
-    if (st != SG_OK) return st;
-    if (plan.n_shares > 1) {
-      st = launch_context_join(a, tab, p.head_dim, p.dtype, s);
+    for (int i = 0; i < plan.n_launches; ++i) {
+      a.part = plan.part[i];
+      const int st = p.dtype == SG_F32            ? launch_context_f32(a, tab, plan.kind[i], p.head_dim, s)
+                     : plan.kind[i] == kCtxWide ? launch_context_bf16_wide(a, tab, p.head_dim, s)
+                                                : launch_context_bf16_split(a, tab, p.head_dim, s);
+      if (st != SG_OK) return st;
+    }
+    if (plan.join) {
+      const int st = launch_context_join(a, tab, p.head_dim, p.dtype, s);
       if (st != SG_OK) return st;
     }
   }

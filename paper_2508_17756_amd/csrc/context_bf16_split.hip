@@ -28,15 +28,31 @@ __device__ __forceinline__ void attend_keys(const Frags& f, const uint32_t kb0, 
                                             const uint64_t valid, RowState<D>& st) {
   static_assert(D == 128 || NB == 2, "");
   constexpr uint64_t kFull = (D == 128 && NB == 1) ? 0xffffffffull : ~0ull;
+  // All fragments of a product are read at once, those of V before the softmax: one wavefront per SIMD has nobody to hide the reads behind.
+  bf16x8 kf[NB][D / 16], vf[2 * NB][D / 32];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+      kf[b][kk] = __builtin_bit_cast(bf16x8, *(const SG_LDS u32x4*)(uintptr_t)(kb0 + f.k[D == 128 ? kk : 4 * b + kk] + (D == 128 ? b * 32 * kSlot : 0)));
+  __builtin_amdgcn_sched_barrier(0);
   f32x16 s[NB];
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const uint32_t at = kb0 + f.k[D == 128 ? kk : 4 * b + kk] + (D == 128 ? b * 32 * kSlot : 0);
-      const bf16x8 x = __builtin_bit_cast(bf16x8, *(const SG_LDS u32x4*)(uintptr_t)at);
-      s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, qf[kk], kk == 0 ? zero16() : s[b], 0, 0, 0);
+    for (int b = 0; b < NB; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][kk], qf[kk], kk == 0 ? zero16() : s[b], 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < 2 * NB; ++i)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const int b = i >> 1, h = i & 1;
+      const uint32_t at = vb0 + f.v[D == 128 ? db : 2 * b + db] + (D == 128 ? b * 32 * kSlot : 0) + h * 16 * kSlot;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)(at + 8 * kSlot));
+      const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      vf[i][db] = __builtin_bit_cast(bf16x8, both);
     }
+  __builtin_amdgcn_sched_barrier(0);
   if (valid != kFull) mask_scores<D, NB>(s, valid);
   float mx = s[0][0];
 #pragma unroll
@@ -72,24 +88,18 @@ __device__ __forceinline__ void attend_keys(const Frags& f, const uint32_t kb0, 
         p[r + 1] = (__bf16)e1;
       }
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        const uint32_t at = vb0 + f.v[D == 128 ? db : 2 * b + db] + (D == 128 ? b * 32 * kSlot : 0) + h * 16 * kSlot;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)at);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)(at + 8 * kSlot));
-        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), p, st.o[db], 0, 0, 0);
-      }
+      for (int db = 0; db < D / 32; ++db) st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * b + h][db], p, st.o[db], 0, 0, 0);
     }
   st.l += sum0 + sum1;
 }
 
 // ------------------------------------------------------------------------------------------------------ few rows
 // A wavefront's LDS: two stages of 32 slots of K and V.  After the keys it holds the wavefront's sums: 32 rows x D floats (16-byte chunk c of
-// row r at chunk c ^ r), then (reference, sum) of the rows.
+// row r at chunk c ^ (r & 15)), then (reference, sum) of the rows and where they go.
 constexpr int kSplitStage = 2 * 32 * kSlot;              // 16 KiB
 constexpr int kSplitWave = 2 * kSplitStage;
 constexpr int kSplitLds = 4 * kSplitWave;
-constexpr int kSumsAt = kSplitStage;
+constexpr int kSumsAt = kSplitStage, kRowsAt = kSumsAt + 512;
 
 template <int D>
 __global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArgs a, const CtxTable tab) {
@@ -100,22 +110,16 @@ __global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArg
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lq = lane & 31, half = lane >> 5;
 
-  const int grid0 = (a.part[0].items + 7) / 8 * 8;
-  const int which = (int)blockIdx.x < grid0 ? 0 : 1;
-  const CtxPart& p = a.part[which];
-  int id = ctx_xcd_order((int)blockIdx.x - (which ? grid0 : 0), p.items);
-  if (id < 0) return;
-  const int row_block = id % p.row_blocks;
-  id /= p.row_blocks;
-  const int split = id % p.splits;
-  id /= p.splits;
-  const int kvh = id % a.kv_heads, batch = id / a.kv_heads;
+  const CtxPart& p = a.part;
+  // The grid names tile and head of keys, so that the table of tiles can be read without waiting for anything else.
+  const int split = (int)blockIdx.x / p.row_blocks, row_block = (int)blockIdx.x - split * p.row_blocks, kvh = (int)blockIdx.y, batch = (int)blockIdx.z;
   if (!p.stacked && a.run && a.run[batch] == 0) return;
   const int way = wave & (p.ways - 1);
   const int row0 = (row_block * (4 / p.ways) + wave / p.ways) * 32;
 
   RowState<D> st;
   clear(st);
+  CtxRowEnd end = {0, 0};   // of row lq
   if (row0 < p.rows) {
     const Segment g0 = segment(a, tab, 0, batch, kvh), g1 = segment(a, tab, 1, batch, kvh);
     const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
@@ -138,7 +142,9 @@ __global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArg
     int j = from + way;
     if (j < to) issue(j, 0);
     bf16x8 qf[D / 16];
-    load_query<D>(a, tab, ctx_row(a, p, batch, kvh, row0 + lq), qf);
+    const CtxRow row = ctx_row(a, p, batch, kvh, row0 + lq);
+    load_query<D>(a, tab, row, qf);
+    end = ctx_row_end<uint16_t>(a, tab, row);
     const Frags f = make_frags();
     const float c_log2 = a.scale * 1.4426950408889634f;
     for (int at = 0; j < to; j += p.ways, at ^= 1) {
@@ -162,41 +168,17 @@ __global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArg
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       const f32x4 x = {st.o[db][4 * g], st.o[db][4 * g + 1], st.o[db][4 * g + 2], st.o[db][4 * g + 3]};
-      *(SG_LDS f32x4*)(uintptr_t)(mine + lq * (D * 4) + (((8 * db + 2 * g + half) ^ (lq & (D / 4 - 1))) << 4)) = x;
+      *(SG_LDS f32x4*)(uintptr_t)(mine + lq * (D * 4) + (((8 * db + 2 * g + half) ^ (lq & 15)) << 4)) = x;
     }
-  if (half == 0) *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + lq * 8) = f32x2{st.m, l};
+  if (half == 0) {
+    *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + lq * 8) = f32x2{st.m, l};
+    *(SG_LDS u32x4*)(uintptr_t)(mine + kRowsAt + lq * 16) = u32x4{(uint32_t)end.out, (uint32_t)(end.out >> 32), (uint32_t)end.rid, 0u};
+  }
   __syncthreads();
   const uint32_t group = lds0 + (wave & ~(p.ways - 1)) * kSplitWave;
-  constexpr int kLanes = D / 4;   // lanes per row: 4 channels each
-  const int rows_at_once = 64 * p.ways / kLanes, tg = way * 64 + lane;
-  const int chunk = tg % kLanes;
-  for (int r = tg / kLanes; r < 32; r += rows_at_once) {
-    if (row0 + r >= p.rows) break;
-    const CtxRow row = ctx_row(a, p, batch, kvh, row0 + r);
-    if (!row.there) continue;
-    float top = -__builtin_inff();
-    for (int w = 0; w < p.ways; ++w) top = fmaxf(top, (*(const SG_LDS f32x2*)(uintptr_t)(group + w * kSplitWave + kSumsAt + r * 8))[0]);
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
-    for (int w = 0; w < p.ways; ++w) {
-      const uint32_t at = group + w * kSplitWave;
-      const f32x2 ml = *(const SG_LDS f32x2*)(uintptr_t)(at + kSumsAt + r * 8);
-      if (ml[1] == 0.f) continue;   // a share without keys (one whose scores are NaN has a reference of -inf too)
-      const float e = __builtin_amdgcn_exp2f(ml[0] - top);
-      sum += e * ml[1];
-      acc += e * *(const SG_LDS f32x4*)(uintptr_t)(at + r * (D * 4) + ((chunk ^ (r & (D / 4 - 1))) << 4));
-    }
-    if (a.n_shares == 1) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      uint16_t* const o = (uint16_t*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 4 * chunk;
-      *(u32x2*)o = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
-    } else {
-      const int64_t at = (int64_t)row.rid * a.n_shares + p.first_share + split;
-      const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
-      *(f32x4*)(a.shares + at * D + 4 * chunk) = acc;
-      if (chunk == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{top, sum};
-    }
-  }
+  if (p.ways == 4) ctx_finish<uint16_t, D, 32, 4>(a, p, group, kSplitWave, kSumsAt, kRowsAt, way, split, row0);
+  else if (p.ways == 2) ctx_finish<uint16_t, D, 32, 2>(a, p, group, kSplitWave, kSumsAt, kRowsAt, way, split, row0);
+  else ctx_finish<uint16_t, D, 32, 1>(a, p, group, kSplitWave, kSumsAt, kRowsAt, way, split, row0);
 }
 
 }  // namespace
@@ -208,14 +190,13 @@ int launch_context_bf16_split(const CtxArgs& a, const CtxTable& tab, int head_di
   constexpr int kMaxDevices = 64;
   static std::atomic<bool> attr_set[kMaxDevices][2];
   auto launch = [&](auto kern, int slot) -> int {
-    const int64_t grid = ((int64_t)a.part[0].items + 7) / 8 * 8 + ((int64_t)a.part[1].items + 7) / 8 * 8;
-    if (grid > (1ll << 31) - 1) return SG_ERR_UNSUPPORTED;
-    if (grid == 0) return SG_OK;
+    if (a.part.items == 0) return SG_OK;
+    const dim3 grid((unsigned)(a.part.row_blocks * a.part.splits), (unsigned)a.kv_heads, (unsigned)(a.part.stacked ? 1 : a.n_tiles));
     if (dev < 0 || dev >= kMaxDevices || !attr_set[dev][slot].load(std::memory_order_acquire)) {
       SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, kSplitLds));
       if (dev >= 0 && dev < kMaxDevices) attr_set[dev][slot].store(true, std::memory_order_release);
     }
-    kern<<<dim3((unsigned)grid), 256, kSplitLds, s>>>(a, tab);
+    kern<<<grid, 256, kSplitLds, s>>>(a, tab);
     SG_HIP_TRY(hipGetLastError());
     return SG_OK;
   };

@@ -30,39 +30,40 @@ __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs
   const uint32_t lds0 = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lq = lane & 31, half = lane >> 5;
-  const CtxPart& p = a.part[0];
+  const CtxPart& p = a.part;
   // Only the tiles that run are numbered, so that the work is spread evenly whichever they are.
-  uint64_t active = a.n_tiles >= 64 ? ~0ull : (1ull << a.n_tiles) - 1;
-  if (a.run) active = __ballot(lane < a.n_tiles && a.run[lane < a.n_tiles ? lane : 0] != 0);
-  const int per_tile = a.kv_heads * p.row_blocks;
+  uint64_t active = p.stacked ? 1 : a.n_tiles >= 64 ? ~0ull : (1ull << a.n_tiles) - 1;
+  if (a.run && !p.stacked) active = __ballot(lane < a.n_tiles && a.run[lane < a.n_tiles ? lane : 0] != 0);
+  const int per_head = p.splits * p.row_blocks, per_tile = a.kv_heads * per_head;
   const int id = ctx_xcd_order((int)blockIdx.x, __builtin_popcountll(active) * per_tile);
   if (id < 0) return;
   const int nth = id / per_tile, in_tile = id - nth * per_tile;
   const int tile = __builtin_amdgcn_readfirstlane(ctx_nth_tile(active, nth));
-  const int kvh = __builtin_amdgcn_readfirstlane(in_tile / p.row_blocks), row_block = in_tile - kvh * p.row_blocks;
+  const int kvh = __builtin_amdgcn_readfirstlane(in_tile / per_head), in_head = in_tile - kvh * per_head;
+  const int split = __builtin_amdgcn_readfirstlane(in_head / p.row_blocks), row_block = in_head - split * p.row_blocks;
   const int row0 = row_block * 128 + wave * 32;
 
   const Segment g0 = segment(a, tab, 0, tile, kvh), g1 = segment(a, tab, 1, tile, kvh);
   const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
-  const int n = n0 + n1;
+  const int from = (int)((int64_t)(n0 + n1) * split / p.splits), n = (int)((int64_t)(n0 + n1) * (split + 1) / p.splits) - from;   // stages: j = 0 is `from`
 
   bool mask_next = true;   // of the stage whose keys are requested next: whether key key0 + lane is unmasked
   auto fetch_mask = [&](int j) SG_INLINE {
-    const int key = (j - n0) * kKeys + lane;
-    mask_next = !(j >= n0 && j < n && g1.mask) || (key < g1.len && g1.mask[key] != 0);
+    const int key = (from + j - n0) * kKeys + lane;
+    mask_next = !(from + j >= n0 && j < n && g1.mask) || (key < g1.len && g1.mask[key] != 0);
   };
   const int first = wave * (kWideSlots<D> / 4);
   auto request = [&](int j, uint64_t v, bool is_v) SG_INLINE {
-    const bool second = j >= n0;
+    const bool second = from + j >= n0;
     const Segment& g = second ? g1 : g0;
-    const int key0 = (second ? j - n0 : j) * kKeys;
+    const int key0 = (second ? from + j - n0 : from + j) * kKeys;
     const uint32_t dst = lds0 + (is_v ? 2 * kHalf : 0) + (j & 1) * kHalf + first * kSlot;
     move_half<D, kInstr>(is_v ? g.v : g.k, g.token, key0, first, v, is_v, dst);
   };
   // which of its keys count
   auto counting = [&](int j) SG_INLINE -> uint64_t {
-    const bool second = j >= n0;
-    const int key0 = (second ? j - n0 : j) * kKeys;
+    const bool second = from + j >= n0;
+    const int key0 = (second ? from + j - n0 : from + j) * kKeys;
     const uint64_t v = __ballot(mask_next && key0 + lane < (second ? g1.len : g0.len));
     if (g1.mask) fetch_mask(j + 1);
     return v;
@@ -253,6 +254,19 @@ __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs
   const uint32_t lu = __float_as_uint(l);
   const auto sw = __builtin_amdgcn_permlane32_swap(lu, lu, false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  const CtxRow mine = ctx_row(a, p, tile, kvh, row0 + lq);
+  if (a.n_shares > 0) {   // a share: sums and reference for the join
+    if (!mine.there) return;
+    const int64_t at = (int64_t)mine.rid * a.n_shares + p.first_share + split;
+    const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
+    if (half == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{m, l};
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(f32x4*)(a.shares + at * D + 32 * db + 8 * g + 4 * half) = f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
+    return;
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   static_assert(4 * 32 * D * 2 <= 2 * kHalf, "rows go through the keys' half of LDS, which nobody reads after the last barrier");
   const uint32_t buf = lds0 + wave * (32 * D * 2);
@@ -264,16 +278,16 @@ __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs
       *(SG_LDS u32x2*)(uintptr_t)(buf + lq * (D * 2) + (((4 * db + g) ^ (lq & (kChunks - 1))) << 4) + 8 * half) = w;
     }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  const CtxRow mine = ctx_row(a, p, tile, kvh, row0 + lq);
-  const int64_t off = (int64_t)mine.head * a.o_head + (int64_t)mine.token * a.o_token;
-  uint16_t* const out = (uint16_t*)tab.out[tile];
+  uint16_t* const place = (uint16_t*)tab.out[mine.tile] + (int64_t)mine.head * a.o_head + (int64_t)mine.token * a.o_token;
+  const uint64_t to = mine.there ? (uint64_t)(uintptr_t)place : 0;   // of the row of lane lq
   const int sub = lane / kChunks, chunk = lane % kChunks;
 #pragma unroll
   for (int i = 0; i < 32 / kRowsPer; ++i) {
     const int r = kRowsPer * i + sub;
-    const int lo = __shfl((int)(uint32_t)off, r, 64), hi = __shfl((int)(off >> 32), r, 64);
+    const uint64_t lo = (uint32_t)__shfl((int)(uint32_t)to, r, 64), hi = (uint32_t)__shfl((int)(uint32_t)(to >> 32), r, 64);
     const u32x4 x = *(const SG_LDS u32x4*)(uintptr_t)(buf + r * (D * 2) + ((chunk ^ (r & (kChunks - 1))) << 4));
-    if (row0 + r < p.rows) *(u32x4*)(out + ((int64_t)hi << 32 | (uint32_t)lo) + 8 * chunk) = x;
+    uint16_t* const dst = (uint16_t*)(uintptr_t)(hi << 32 | lo);
+    if (dst) *(u32x4*)(dst + 8 * chunk) = x;
   }
 }
 
@@ -285,7 +299,7 @@ int launch_context_bf16_wide(const CtxArgs& a, const CtxTable& tab, int head_dim
   constexpr int kMaxDevices = 64;
   static std::atomic<bool> attr_set[kMaxDevices][2];   // the kernels' dynamic-LDS limit has been raised
   auto launch = [&](auto kern, int slot, int lds) -> int {
-    const int64_t grid = ((int64_t)a.part[0].items + 7) / 8 * 8;
+    const int64_t grid = ((int64_t)a.part.items + 7) / 8 * 8;
     if (grid == 0) return SG_OK;
     if (dev < 0 || dev >= kMaxDevices || !attr_set[dev][slot].load(std::memory_order_acquire)) {
       SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));

@@ -23,17 +23,17 @@ struct CtxTable {
   void* out[kCtxTilesPerLaunch];
 };
 
-// One way of numbering (rows, shares of the keys): `items` workgroups.  Stacked: the rows of all tiles behind one another over segment 0 alone.
+// One launch's work: (rows, shares of the keys) in `items` workgroups.
 struct CtxPart {
   int32_t items;
-  int32_t batches;       // tiles, or 1 if stacked
-  int32_t rows;          // rows of a batch and head of keys
-  int32_t row_blocks;    // groups of row blocks (what one workgroup takes) of a batch and head of keys
+  int32_t rows;          // of a batch and head of keys; a batch is a tile, or all tiles if stacked
+  int32_t row_blocks;    // what one workgroup takes of them
   int32_t splits;        // shares of the keys taken by different workgroups
   int32_t ways;          // shares of the keys inside a workgroup (its other wavefronts take other row blocks): 1, 2, 4
-  int32_t first_share;   // place of its first share among the shares that are joined
+  int32_t first_share;   // place of its first share among a row's shares in the workspace
+  int32_t prior;         // shares of a row that an earlier launch left there and this one joins with its own: its results are final
   int32_t seg0, seg1;    // segments it attends
-  int32_t stacked;
+  int32_t stacked;       // the rows of all tiles behind one another
 };
 
 struct CtxArgs {
@@ -48,9 +48,9 @@ struct CtxArgs {
   float* shares;          // workspace: [row][share][head_dim] sums of p v, then [row][share][2] (reference, sum of p)
   int32_t cap0, cap1;     // rows in the buffers
   int32_t heads, kv_heads, group, tokens, n_tiles;
-  int32_t n_shares;       // per row; 1: the result is written directly
+  int32_t n_shares;       // per row, in the workspace; 0: none, results are written directly
   float scale;
-  CtxPart part[2];
+  CtxPart part;
 };
 
 // Rows that no key transfer may read: the source of what is not to count.
@@ -92,20 +92,119 @@ __device__ __forceinline__ CtxRow ctx_row(const CtxArgs& a, const CtxPart& p, in
   if (p.stacked && a.run) r.there = r.there && a.run[r.tile] != 0;
   return r;
 }
+// What the end of a call needs of a row: found once (divisions), kept in registers over the keys, then passed on in LDS.
+struct CtxRowEnd {
+  uint64_t out;   // address of its output; 0: it is not there
+  int rid;
+};
+template <typename T>
+__device__ __forceinline__ CtxRowEnd ctx_row_end(const CtxArgs& a, const CtxTable& tab, const CtxRow& r) {
+  T* const o = (T*)tab.out[r.tile] + (int64_t)r.head * a.o_head + (int64_t)r.token * a.o_token;
+  return {r.there ? (uint64_t)(uintptr_t)o : 0, r.rid};
+}
+
+// A row's shares in the workspace, (reference in the log2 domain, sum of probabilities) and sums of p v, joined to what (top, sum, acc) holds: four
+// channels a lane.  The loads of 16 shares are in flight together; one share after the other, 32 of them took 25 us.
+__device__ __forceinline__ void ctx_add_shares(const f32x2* ml, const float* sums, int64_t stride, int n, float& top, float& sum, f32x4& acc) {
+  constexpr int kBatch = 16;
+  for (int k = 0; k < n; k += kBatch) {
+    f32x2 x[kBatch];
+    f32x4 v[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int i = k + u < n ? k + u : n - 1;
+      x[u] = ml[i];
+      v[u] = *(const f32x4*)(sums + i * stride);
+    }
+    float most = top;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) most = fmaxf(most, x[u][0]);
+    const float keep = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - most);
+    top = most;
+    sum *= keep;
+    acc *= keep;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      // a share without keys counts for nothing (one whose scores are all NaN has a reference of -inf as well, but a sum)
+      const float e = k + u >= n || x[u][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[u][0] - top);
+      sum += e * x[u][1];
+      acc += e * v[u];
+    }
+  }
+}
+
+// The end of a call whose wavefronts attended shares of the keys.  A wavefront's LDS holds its sums, ROWS x D floats (16-byte chunk c of row r at chunk
+// c ^ (r & 15)), at `sums` (reference in the log2 domain, sum) of the rows and at `ends` their CtxRowEnd.  The WAYS wavefronts of a row block join
+// their shares, and those of an earlier launch, and write the results or, for a later join, their share.  Four rows at a time, so that their reads
+// overlap: one after the other, 32 rows took 5 us.
+template <typename OUT, int D, int ROWS, int WAYS>
+__device__ __forceinline__ void ctx_finish(const CtxArgs& a, const CtxPart& p, uint32_t group, uint32_t wave_bytes, uint32_t sums, uint32_t ends,
+                                           int way, int split, int row0) {
+  constexpr int kLanes = D / 4, kAtOnce = 64 * WAYS / kLanes, kSteps = ROWS / kAtOnce > 0 ? ROWS / kAtOnce : 1, kBatch = kSteps < 4 ? kSteps : 4;
+  const int tg = way * 64 + (threadIdx.x & 63), chunk = tg % kLanes, first = tg / kLanes;
+  const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
+  for (int step = 0; step < kSteps && row0 + step * kAtOnce < p.rows; step += kBatch) {
+    u32x4 end[kBatch];
+    f32x2 ml[kBatch][WAYS];
+    f32x4 o[kBatch][WAYS];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int r = first + (step + i) * kAtOnce;
+      if (ROWS >= kAtOnce || r < ROWS) {
+        end[i] = *(const SG_LDS u32x4*)(uintptr_t)(group + ends + r * 16);
+#pragma unroll
+        for (int w = 0; w < WAYS; ++w) {
+          ml[i][w] = *(const SG_LDS f32x2*)(uintptr_t)(group + w * wave_bytes + sums + r * 8);
+          o[i][w] = *(const SG_LDS f32x4*)(uintptr_t)(group + w * wave_bytes + r * (D * 4) + ((chunk ^ (r & 15)) << 4));
+        }
+      } else {
+        end[i] = u32x4{0, 0, 0, 0};
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const uint64_t to = (uint64_t)end[i][1] << 32 | end[i][0];
+      if (!to) continue;
+      float top = ml[i][0][0], sum = 0.f;
+#pragma unroll
+      for (int w = 1; w < WAYS; ++w) top = fmaxf(top, ml[i][w][0]);
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < WAYS; ++w) {
+        const float e = ml[i][w][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[i][w][0] - top);   // 0: no keys (NaN scores leave a sum)
+        sum += e * ml[i][w][1];
+        acc += e * o[i][w];
+      }
+      const int64_t shares = (int64_t)(int)end[i][2] * a.n_shares;
+      if (p.prior) ctx_add_shares((const f32x2*)(a.shares + all * D) + shares, a.shares + shares * D + 4 * chunk, D, p.prior, top, sum, acc);
+      if (a.n_shares == p.prior) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if constexpr (sizeof(OUT) == 4) *(f32x4*)((OUT*)(uintptr_t)to + 4 * chunk) = acc * inv;
+        else *(u32x2*)((OUT*)(uintptr_t)to + 4 * chunk) = u32x2{pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv)};
+      } else {
+        const int64_t at = shares + p.first_share + split;
+        *(f32x4*)(a.shares + at * D + 4 * chunk) = acc;
+        if (chunk == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{top, sum};
+      }
+    }
+  }
+}
 
 // ---------------------------------------------------------------------------------------------------- host side
-// The launches of one call (at most kCtxTilesPerLaunch tiles each) and what they need of the workspace.
+// The launches for at most kCtxTilesPerLaunch tiles and what they need of the workspace.
+enum { kCtxWide, kCtxSplit, kCtxSplit16 };   // workgroups of 128 rows that share their keys; wavefronts of 32 (fp32: or 16) rows with keys of their own
 struct CtxPlan {
-  bool wide;             // workgroups of 128 rows share their keys in LDS, nothing is split
-  int32_t wave_rows;     // otherwise rows of a wavefront: 32 (fp32: or 16)
-  int32_t n_shares;
+  int32_t n_launches;
+  int32_t kind[2];
   CtxPart part[2];
+  bool join;             // a last launch joins the shares
+  int32_t n_shares;
   size_t bytes;          // workspace
 };
 CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles);
 int launch_context_bf16_wide(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s);
 int launch_context_bf16_split(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s);
-int launch_context_f32(const CtxArgs& a, const CtxTable& tab, const CtxPlan& plan, int head_dim, hipStream_t s);
+int launch_context_f32(const CtxArgs& a, const CtxTable& tab, int kind, int head_dim, hipStream_t s);
 int launch_context_join(const CtxArgs& a, const CtxTable& tab, int head_dim, int dtype, hipStream_t s);
 
 }  // namespace sg

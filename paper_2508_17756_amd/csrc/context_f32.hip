@@ -18,9 +18,9 @@ namespace {
 
 #define SG_INLINE __attribute__((always_inline))
 
-// A wavefront's LDS: two stages of 8 KiB of keys and 8 KiB of values; after the keys its sums (rows x D floats), then (reference, sum).
+// A wavefront's LDS: two stages of 8 KiB of keys and 8 KiB of values; after the keys its sums (rows x D floats), then (reference, sum) of the rows and where they go.
 constexpr int kHalfStage = 8192, kStage = 2 * kHalfStage, kWaveLds = 2 * kStage, kLds = 4 * kWaveLds;
-constexpr int kSumsAt = kStage;
+constexpr int kSumsAt = kStage, kRowsAt = kSumsAt + 512;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Segment {
@@ -69,16 +69,23 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lq = lane & 15, grp = lane >> 4;
 
-  const int grid0 = (a.part[0].items + 7) / 8 * 8;
-  const int which = (int)blockIdx.x < grid0 ? 0 : 1;
-  const CtxPart& p = a.part[which];
-  int id = ctx_xcd_order((int)blockIdx.x - (which ? grid0 : 0), p.items);
-  if (id < 0) return;
-  const int row_block = id % p.row_blocks;
-  id /= p.row_blocks;
-  const int split = id % p.splits;
-  id /= p.splits;
-  const int kvh = id % a.kv_heads, batch = id / a.kv_heads;
+  const CtxPart& p = a.part;
+  int split, row_block, kvh, batch;
+  if constexpr (SHARED) {
+    int id = ctx_xcd_order((int)blockIdx.x, p.items);
+    if (id < 0) return;
+    row_block = id % p.row_blocks;
+    id /= p.row_blocks;
+    split = id % p.splits;
+    id /= p.splits;
+    kvh = id % a.kv_heads;
+    batch = id / a.kv_heads;
+  } else {   // the grid names tile and head of keys, so that the table of tiles can be read without waiting for anything else
+    split = (int)blockIdx.x / p.row_blocks;
+    row_block = (int)blockIdx.x - split * p.row_blocks;
+    kvh = (int)blockIdx.y;
+    batch = (int)blockIdx.z;
+  }
   if (!p.stacked && a.run && a.run[batch] == 0) return;
   const int way = wave & (p.ways - 1);
   const int row0 = (row_block * (4 / p.ways) + wave / p.ways) * kRows;
@@ -93,6 +100,9 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const 
     m[qb] = -__builtin_inff();
     l[qb] = 0.f;
   }
+  CtxRowEnd end[QB];   // of the rows lq
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) end[qb] = {0, 0};
   if (SHARED || row0 < p.rows) {
     const Segment g0 = segment(a, tab, 0, batch, kvh), g1 = segment(a, tab, 1, batch, kvh);
     const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
@@ -140,6 +150,7 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const 
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const CtxRow row = ctx_row(a, p, batch, kvh, row0 + 16 * qb + lq);
+      end[qb] = ctx_row_end<float>(a, tab, row);
       const float* const src = (const float*)tab.q[row.tile] + (int64_t)row.head * a.q_head + (int64_t)row.token * a.q_token;
 #pragma unroll
       for (int jj = 0; jj < D / 16; ++jj) {
@@ -247,14 +258,22 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const 
   if constexpr (SHARED) {
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      if (row0 + 16 * qb + lq >= p.rows) continue;
-      const CtxRow row = ctx_row(a, p, batch, kvh, row0 + 16 * qb + lq);
-      float* const dst = (float*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 16 * grp;
-      const float inv = l[qb] == 0.f ? 0.f : 1.f / l[qb];
+      if (!end[qb].out) continue;
+      float* dst;
+      float by = 1.f;
+      if (a.n_shares == 0) {
+        dst = (float*)(uintptr_t)end[qb].out + 16 * grp;
+        by = l[qb] == 0.f ? 0.f : 1.f / l[qb];
+      } else {
+        const int64_t at = (int64_t)end[qb].rid * a.n_shares + p.first_share + split;
+        const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
+        dst = a.shares + at * D + 16 * grp;
+        if (grp == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{m[qb] * kLog2e, l[qb]};
+      }
 #pragma unroll
       for (int h = 0; h < D / 64; ++h)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) *(f32x4*)(dst + 64 * h + 4 * r) = four(qb, h, r) * inv;
+        for (int r = 0; r < 4; ++r) *(f32x4*)(dst + 64 * h + 4 * r) = four(qb, h, r) * by;
     }
   } else {
     // ---- join of the shares in this workgroup; chunk c of row r at chunk c ^ (r & 15)
@@ -266,63 +285,41 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const 
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           *(SG_LDS f32x4*)(uintptr_t)(mine + (16 * qb + lq) * (D * 4) + (((16 * h + 4 * grp + r) ^ lq) << 4)) = four(qb, h, r);
-      if (grp == 0) *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + (16 * qb + lq) * 8) = f32x2{m[qb], l[qb]};
+      if (grp == 0) {
+        *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + (16 * qb + lq) * 8) = f32x2{m[qb] * kLog2e, l[qb]};
+        *(SG_LDS u32x4*)(uintptr_t)(mine + kRowsAt + (16 * qb + lq) * 16) = u32x4{(uint32_t)end[qb].out, (uint32_t)(end[qb].out >> 32), (uint32_t)end[qb].rid, 0u};
+      }
     }
     __syncthreads();
     const uint32_t group = lds0 + (wave & ~(p.ways - 1)) * kWaveLds;
-    const int rows_at_once = 64 * p.ways / kChunks, tg = way * 64 + lane;
-    const int chunk = tg % kChunks;
-    for (int r = tg / kChunks; r < kRows; r += rows_at_once) {
-      if (row0 + r >= p.rows) break;
-      const CtxRow row = ctx_row(a, p, batch, kvh, row0 + r);
-      if (!row.there) continue;
-      float top = -__builtin_inff();
-      for (int w = 0; w < p.ways; ++w) top = fmaxf(top, (*(const SG_LDS f32x2*)(uintptr_t)(group + w * kWaveLds + kSumsAt + r * 8))[0]);
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      float sum = 0.f;
-      for (int w = 0; w < p.ways; ++w) {
-        const uint32_t at = group + w * kWaveLds;
-        const f32x2 ml = *(const SG_LDS f32x2*)(uintptr_t)(at + kSumsAt + r * 8);
-        if (ml[1] == 0.f) continue;   // a share without keys (one whose scores are NaN has a reference of -inf too)
-        const float e = __builtin_amdgcn_exp2f((ml[0] - top) * kLog2e);
-        sum += e * ml[1];
-        acc += e * *(const SG_LDS f32x4*)(uintptr_t)(at + r * (D * 4) + ((chunk ^ (r & 15)) << 4));
-      }
-      if (a.n_shares == 1) {
-        float* const dst = (float*)tab.out[row.tile] + (int64_t)row.head * a.o_head + (int64_t)row.token * a.o_token + 4 * chunk;
-        *(f32x4*)dst = sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc / sum;
-      } else {
-        const int64_t at = (int64_t)row.rid * a.n_shares + p.first_share + split;
-        const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
-        *(f32x4*)(a.shares + at * D + 4 * chunk) = acc;
-        if (chunk == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{top * kLog2e, sum};
-      }
-    }
+    if (p.ways == 4) ctx_finish<float, D, kRows, 4>(a, p, group, kWaveLds, kSumsAt, kRowsAt, way, split, row0);
+    else if (p.ways == 2) ctx_finish<float, D, kRows, 2>(a, p, group, kWaveLds, kSumsAt, kRowsAt, way, split, row0);
+    else ctx_finish<float, D, kRows, 1>(a, p, group, kWaveLds, kSumsAt, kRowsAt, way, split, row0);
   }
 }
 
 }  // namespace
 
-int launch_context_f32(const CtxArgs& a, const CtxTable& tab, const CtxPlan& plan, int head_dim, hipStream_t s) {
+int launch_context_f32(const CtxArgs& a, const CtxTable& tab, int kind, int head_dim, hipStream_t s) {
   int dev = 0;
   SG_HIP_TRY(hipGetDevice(&dev));
   constexpr int kMaxDevices = 64;
   static std::atomic<bool> attr_set[kMaxDevices][6];   // the kernels' dynamic-LDS limit has been raised
   auto launch = [&](auto kern, int slot, int lds) -> int {
-    const int64_t grid = ((int64_t)a.part[0].items + 7) / 8 * 8 + ((int64_t)a.part[1].items + 7) / 8 * 8;
-    if (grid > (1ll << 31) - 1) return SG_ERR_UNSUPPORTED;
-    if (grid == 0) return SG_OK;
+    if (a.part.items == 0) return SG_OK;
+    const dim3 grid = kind == kCtxWide ? dim3((unsigned)((a.part.items + 7) / 8 * 8))
+                                       : dim3((unsigned)(a.part.row_blocks * a.part.splits), (unsigned)a.kv_heads, (unsigned)(a.part.stacked ? 1 : a.n_tiles));
     if (dev < 0 || dev >= kMaxDevices || !attr_set[dev][slot].load(std::memory_order_acquire)) {
       SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
       if (dev >= 0 && dev < kMaxDevices) attr_set[dev][slot].store(true, std::memory_order_release);
     }
-    kern<<<dim3((unsigned)grid), 256, lds, s>>>(a, tab);
+    kern<<<grid, 256, lds, s>>>(a, tab);
     SG_HIP_TRY(hipGetLastError());
     return SG_OK;
   };
-  if (plan.wide)
+  if (kind == kCtxWide)
     return head_dim == 128 ? launch(context_f32_kernel<128, 2, true>, 4, kWaveLds) : launch(context_f32_kernel<64, 2, true>, 5, kWaveLds);
-  if (plan.wave_rows == 16)
+  if (kind == kCtxSplit16)
     return head_dim == 128 ? launch(context_f32_kernel<128, 1, false>, 0, kLds) : launch(context_f32_kernel<64, 1, false>, 1, kLds);
   return head_dim == 128 ? launch(context_f32_kernel<128, 2, false>, 2, kLds) : launch(context_f32_kernel<64, 2, false>, 3, kLds);
 }

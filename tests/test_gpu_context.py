@@ -57,6 +57,18 @@ def test_prefix_sizes(dtype, d, tiles, tokens, heads, kv_heads, own, prefix):
 
 
 @pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tiles, tokens, heads, kv_heads, own, prefix", [
+    (20, 1, 10, 2, 0, 130), (20, 1, 10, 2, 31, 1300), (33, 4, 2, 1, 0, 900), (40, 1, 16, 4, 700, 2000), (17, 8, 2, 1, 64, 128), (64, 16, 1, 1, 5, 640),
+    (13, 5, 6, 6, 2000, 700)])
+def test_prefix_of_more_stacked_rows_than_a_wavefront_takes(dtype, d, tiles, tokens, heads, kv_heads, own, prefix):
+    for length in (None, prefix // 3):
+        c = Call(tiles, tokens, heads, kv_heads, d, dtype, prefix, own=own, prefix=True, lay="token", ragged=own > 0, run=True, seed=own + prefix)
+        c.prefix_len = None if length is None else torch.tensor([length], dtype=torch.int32)
+        _run(c)
+
+
+@pytest.mark.parametrize("dtype", DT)
 @pytest.mark.parametrize("lay", ["packed", "token", "odd"])
 @pytest.mark.parametrize("tokens", [1, 30])
 def test_prefix_strides_lengths_and_skipped_tiles(dtype, lay, tokens):
