@@ -97,12 +97,15 @@ static int attend(const sg_context_problem& p, bool prefix, int n_tiles, const v
     a.cap1 = tile_keys;
     a.heads = p.heads; a.kv_heads = p.kv_heads; a.group = p.heads / p.kv_heads; a.tokens = p.tokens; a.n_tiles = n;
     a.n_shares = plan.n_shares;
+    a.by_tokens = make_divisor((uint32_t)a.tokens);
+    a.by_rows = make_divisor((uint32_t)(a.group * a.tokens));
     a.scale = p.scale;
     for (int i = 0; i < plan.n_launches; ++i) {
       a.part = plan.part[i];
-      const int st = p.dtype == SG_F32            ? launch_context_f32(a, tab, plan.kind[i], p.head_dim, s)
-                     : plan.kind[i] == kCtxWide ? launch_context_bf16_wide(a, tab, p.head_dim, s)
-                                                : launch_context_bf16_split(a, tab, p.head_dim, s);
+      const int st = p.dtype == SG_F32                ? launch_context_f32(a, tab, plan.kind[i], p.head_dim, s)
+                     : plan.kind[i] == kCtxResident ? launch_context_bf16_resident(a, tab, p.head_dim, s)
+                     : plan.kind[i] == kCtxWide     ? launch_context_bf16_wide(a, tab, p.head_dim, s)
+                                                    : launch_context_bf16_split(a, tab, p.head_dim, s);
       if (st != SG_OK) return st;
     }
     if (plan.join) {

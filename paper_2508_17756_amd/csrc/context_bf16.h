@@ -11,6 +11,13 @@ namespace {
 
 #define SG_INLINE __attribute__((always_inline))
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// How far a score may pass a row's reference, log2, before the reference moves: any reference gives the same quotient, the sums of p v grow to at most
+// 32 times what they are against the maximum, and the common path rescales nothing.  Probabilities are rounded to bf16 for the second product (half
+// a step of each, which averages out over a row); their sum is taken of the rounded ones, so that the weights sum to one.
+constexpr float kSlack = 5.f;
+
 constexpr int kSlot = 256;   // LDS bytes of a "slot": one key of head_dim 128, two neighbouring ones of head_dim 64
 
 __device__ __forceinline__ f32x16 zero16() {
@@ -53,16 +60,13 @@ __device__ __forceinline__ void mask_scores(f32x16 (&s)[NB], const uint64_t vali
     }
 }
 
+// (a row that is not there stands in for the last one; its results are not written)
 template <int D>
 __device__ __forceinline__ void load_query(const CtxArgs& a, const CtxTable& tab, const CtxRow& row, bf16x8 (&qf)[D / 16]) {
   const int half = (threadIdx.x & 63) >> 5;
   const uint16_t* const q = (const uint16_t*)tab.q[row.tile] + (int64_t)row.head * a.q_head + (int64_t)row.token * a.q_token;
 #pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) {
-    u32x4 x = *(const u32x4*)(q + 16 * kk + 8 * half);
-    if (!row.there) x = u32x4{0, 0, 0, 0};
-    qf[kk] = __builtin_bit_cast(bf16x8, x);
-  }
+  for (int kk = 0; kk < D / 16; ++kk) qf[kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(q + 16 * kk + 8 * half));
 }
 
 // The keys of one segment as a stage of 64 (or 32) is taken from them.
@@ -116,6 +120,115 @@ __device__ __forceinline__ void move_half(const char* base, const uint32_t token
       lane_source<D>(first + 4 * u + (lane >> 4), lane, is_v, key, chunk);
       dma16_addr((valid >> key) & 1 ? from + ((uint32_t)key * token + (uint32_t)chunk * 16) : zeros + chunk * 16, dst + u * 1024);
     }
+  }
+}
+
+// One row's softmax (the same in lanes l and l ^ 32) and its output accumulators.
+template <int D>
+struct RowState {
+  f32x16 o[D / 32];
+  float m;   // running maximum, log2 domain
+  float l;   // this lane's share of the sum
+};
+template <int D>
+__device__ __forceinline__ void clear(RowState<D>& st) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
+  st.m = -__builtin_inff();
+  st.l = 0.f;
+}
+
+// NB blocks of 32 keys, K at LDS address kb0 and V at vb0.  head_dim 128: block b is the slots 32 b .. 32 b + 31; head_dim 64: the 32 slots
+// hold two keys each and block b (of 2) is their b-th ones.
+template <int D, int NB>
+__device__ __forceinline__ void attend_keys(const Frags& f, const uint32_t kb0, const uint32_t vb0, const bf16x8 (&qf)[D / 16], const float c_log2,
+                                            const uint64_t valid, RowState<D>& st) {
+  // All fragments of a product are read at once, those of V before the softmax: one or two wavefronts on a SIMD hide little behind each other.
+  static_assert(D == 128 || NB == 2, "");
+  constexpr uint64_t kFull = (D == 128 && NB == 1) ? 0xffffffffull : ~0ull;
+  bf16x8 kf[NB][D / 16], vf[2 * NB][D / 32];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+      kf[b][kk] = __builtin_bit_cast(bf16x8, *(const SG_LDS u32x4*)(uintptr_t)(kb0 + f.k[D == 128 ? kk : 4 * b + kk] + (D == 128 ? b * 32 * kSlot : 0)));
+  __builtin_amdgcn_sched_barrier(0);
+  f32x16 s[NB];
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][kk], qf[kk], kk == 0 ? zero16() : s[b], 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < 2 * NB; ++i)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+      const int b = i >> 1, h = i & 1;
+      const uint32_t at = vb0 + f.v[D == 128 ? db : 2 * b + db] + (D == 128 ? b * 32 * kSlot : 0) + h * 16 * kSlot;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)at);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)(at + 8 * kSlot));
+      const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      vf[i][db] = __builtin_bit_cast(bf16x8, both);
+    }
+  __builtin_amdgcn_sched_barrier(0);
+  if (valid != kFull) mask_scores<D, NB>(s, valid);
+  float mx = s[0][0];
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[b][r]), s[b][r + 1]);
+  const uint32_t mu = __float_as_uint(mx);
+  const auto sw = __builtin_amdgcn_permlane32_swap(mu, mu, false, false);
+  mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+  mx *= c_log2;
+  if (__any(mx > st.m + kSlack)) {   // (the first keys, too: -inf + 5)
+    const float top = mx > st.m + kSlack ? mx : st.m;
+    const float alpha = __builtin_amdgcn_exp2f(top == st.m ? 0.f : st.m - top);   // first keys: exp2(-inf) = 0
+    st.m = top;
+    st.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) st.o[db] *= alpha;
+  }
+  const float neg = st.m == -__builtin_inff() ? 0.f : -st.m;   // no key so far: probabilities 0
+  const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+  float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 p;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) p[r] = (__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], c_log2, neg));
+#pragma unroll
+      for (int r = 0; r < 8; r += 2) {
+        const bf16x2 two = {p[r], p[r + 1]};
+        if (r & 2) sum1 = __builtin_amdgcn_fdot2_f32_bf16(two, ones, sum1, false);
+        else sum0 = __builtin_amdgcn_fdot2_f32_bf16(two, ones, sum0, false);
+      }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * b + h][db], p, st.o[db], 0, 0, 0);
+    }
+  st.l += sum0 + sum1;
+}
+
+// Row lq of lanes lq and lq + 32 to its place (0: none): the two exchange halves, so that each writes 16 bytes at a time.  (Through LDS a store
+// writes whole rows, but the way there and back, with the rows' addresses, took 1,700 cycles; this takes 500.)
+template <int D>
+__device__ __forceinline__ void write_row(const f32x16 (&o)[D / 32], const float inv, const uint64_t to) {
+  const int half = (threadIdx.x & 63) >> 5;
+  uint16_t* const dst = (uint16_t*)(uintptr_t)to + 8 * half;
+  u32x4 w[D / 16];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = 8 * k;   // registers r .. r + 3: channels 32 db + 16 k + 4 half + 0..3, r + 4 .. r + 7: 8 channels on
+      const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[db][r] * inv, o[db][r + 1] * inv), pack_bf16x2(o[db][r + 4] * inv, o[db][r + 5] * inv), false, false);
+      const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16x2(o[db][r + 2] * inv, o[db][r + 3] * inv), pack_bf16x2(o[db][r + 6] * inv, o[db][r + 7] * inv), false, false);
+      w[2 * db + k] = u32x4{(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
+    }
+  if (to) {
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) *(u32x4*)(dst + 16 * i) = w[i];
   }
 }
 

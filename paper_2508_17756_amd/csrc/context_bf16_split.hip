@@ -6,94 +6,6 @@
 namespace sg {
 namespace {
 
-// One row's softmax (the same in lanes l and l ^ 32) and its output accumulators.
-template <int D>
-struct RowState {
-  f32x16 o[D / 32];
-  float m;   // running maximum, log2 domain
-  float l;   // this lane's share of the sum
-};
-template <int D>
-__device__ __forceinline__ void clear(RowState<D>& st) {
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db) st.o[db] = zero16();
-  st.m = -__builtin_inff();
-  st.l = 0.f;
-}
-
-// NB blocks of 32 keys, K at LDS address kb0 and V at vb0.  head_dim 128: block b is the slots 32 b .. 32 b + 31; head_dim 64: the 32 slots
-// hold two keys each and block b (of 2) is their b-th ones.
-template <int D, int NB>
-__device__ __forceinline__ void attend_keys(const Frags& f, const uint32_t kb0, const uint32_t vb0, const bf16x8 (&qf)[D / 16], const float c_log2,
-                                            const uint64_t valid, RowState<D>& st) {
-  static_assert(D == 128 || NB == 2, "");
-  constexpr uint64_t kFull = (D == 128 && NB == 1) ? 0xffffffffull : ~0ull;
-  // All fragments of a product are read at once, those of V before the softmax: one wavefront per SIMD has nobody to hide the reads behind.
-  bf16x8 kf[NB][D / 16], vf[2 * NB][D / 32];
-#pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-      kf[b][kk] = __builtin_bit_cast(bf16x8, *(const SG_LDS u32x4*)(uintptr_t)(kb0 + f.k[D == 128 ? kk : 4 * b + kk] + (D == 128 ? b * 32 * kSlot : 0)));
-  __builtin_amdgcn_sched_barrier(0);
-  f32x16 s[NB];
-#pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-    for (int b = 0; b < NB; ++b) s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][kk], qf[kk], kk == 0 ? zero16() : s[b], 0, 0, 0);
-#pragma unroll
-  for (int i = 0; i < 2 * NB; ++i)
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) {
-      const int b = i >> 1, h = i & 1;
-      const uint32_t at = vb0 + f.v[D == 128 ? db : 2 * b + db] + (D == 128 ? b * 32 * kSlot : 0) + h * 16 * kSlot;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)at);
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SG_LDS s16x4*)(uintptr_t)(at + 8 * kSlot));
-      const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      vf[i][db] = __builtin_bit_cast(bf16x8, both);
-    }
-  __builtin_amdgcn_sched_barrier(0);
-  if (valid != kFull) mask_scores<D, NB>(s, valid);
-  float mx = s[0][0];
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
-  const uint32_t mu = __float_as_uint(mx);
-  const auto sw = __builtin_amdgcn_permlane32_swap(mu, mu, false, false);
-  mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-  const float top = fmaxf(st.m, mx * c_log2);
-  if (__any(top != st.m)) {
-    const float alpha = st.m == top ? 1.f : __builtin_amdgcn_exp2f(st.m - top);   // first keys: exp2(-inf) = 0
-    st.m = top;
-    st.l *= alpha;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) st.o[db] *= alpha;
-  }
-  const float ref = st.m == -__builtin_inff() ? 0.f : st.m;   // no key so far: probabilities 0
-  // The probabilities are rounded to bf16 for the second product (2^-9 of each, which averages out over a row); their sum is taken before.
-  float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-  for (int b = 0; b < NB; ++b)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      bf16x8 p;
-#pragma unroll
-      for (int r = 0; r < 8; r += 2) {
-        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r], c_log2, -ref));
-        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][8 * h + r + 1], c_log2, -ref));
-        sum0 += e0;
-        sum1 += e1;
-        p[r] = (__bf16)e0;
-        p[r + 1] = (__bf16)e1;
-      }
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * b + h][db], p, st.o[db], 0, 0, 0);
-    }
-  st.l += sum0 + sum1;
-}
-
-// ------------------------------------------------------------------------------------------------------ few rows
 // A wavefront's LDS: two stages of 32 slots of K and V.  After the keys it holds the wavefront's sums: 32 rows x D floats (16-byte chunk c of
 // row r at chunk c ^ (r & 15)), then (reference, sum) of the rows and where they go.
 constexpr int kSplitStage = 2 * 32 * kSlot;              // 16 KiB

@@ -19,10 +19,6 @@ constexpr int kWideHalf = kWideSlots<D> * kSlot;   // keys (or values) of a stag
 template <int D>
 constexpr int kWideLds = 4 * kWideHalf<D>;         // two stages of keys, two of values
 
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-constexpr float kSlack = 5.f;   // log2: how far a score may pass the reference before the reference moves
-
 template <int D>
 __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs a, const CtxTable tab) {
   constexpr int kKeys = 64, kInstr = kWideSlots<D> / 16, kHalf = kWideHalf<D>;
@@ -249,8 +245,6 @@ __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // ---- rows go out through LDS (8 KiB a wavefront), so that a store writes whole rows; chunk c of row r sits at chunk c ^ (r % kChunks)
-  constexpr int kChunks = D / 8, kRowsPer = 64 / kChunks;
   const uint32_t lu = __float_as_uint(l);
   const auto sw = __builtin_amdgcn_permlane32_swap(lu, lu, false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
@@ -267,28 +261,7 @@ __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs
         *(f32x4*)(a.shares + at * D + 32 * db + 8 * g + 4 * half) = f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
     return;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  static_assert(4 * 32 * D * 2 <= 2 * kHalf, "rows go through the keys' half of LDS, which nobody reads after the last barrier");
-  const uint32_t buf = lds0 + wave * (32 * D * 2);
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const u32x2 w = {pack_bf16x2(o[db][4 * g] * inv, o[db][4 * g + 1] * inv), pack_bf16x2(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv)};
-      *(SG_LDS u32x2*)(uintptr_t)(buf + lq * (D * 2) + (((4 * db + g) ^ (lq & (kChunks - 1))) << 4) + 8 * half) = w;
-    }
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  uint16_t* const place = (uint16_t*)tab.out[mine.tile] + (int64_t)mine.head * a.o_head + (int64_t)mine.token * a.o_token;
-  const uint64_t to = mine.there ? (uint64_t)(uintptr_t)place : 0;   // of the row of lane lq
-  const int sub = lane / kChunks, chunk = lane % kChunks;
-#pragma unroll
-  for (int i = 0; i < 32 / kRowsPer; ++i) {
-    const int r = kRowsPer * i + sub;
-    const uint64_t lo = (uint32_t)__shfl((int)(uint32_t)to, r, 64), hi = (uint32_t)__shfl((int)(uint32_t)(to >> 32), r, 64);
-    const u32x4 x = *(const SG_LDS u32x4*)(uintptr_t)(buf + r * (D * 2) + ((chunk ^ (r & (kChunks - 1))) << 4));
-    uint16_t* const dst = (uint16_t*)(uintptr_t)(hi << 32 | lo);
-    if (dst) *(u32x4*)(dst + 8 * chunk) = x;
-  }
+  write_row<D>(o, l == 0.f ? 0.f : 1.f / l, ctx_row_end<uint16_t>(a, tab, mine).out);
 }
 
 }  // namespace

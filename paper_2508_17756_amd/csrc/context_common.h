@@ -50,6 +50,7 @@ struct CtxArgs {
   int32_t heads, kv_heads, group, tokens, n_tiles;
   int32_t n_shares;       // per row, in the workspace; 0: none, results are written directly
   float scale;
+  Divisor by_tokens, by_rows;   // tokens, group * tokens
   CtxPart part;
 };
 
@@ -83,9 +84,9 @@ __device__ __forceinline__ CtxRow ctx_row(const CtxArgs& a, const CtxPart& p, in
   r.there = row < p.rows;
   const int c = r.there ? row : p.rows - 1;
   const int per = a.group * a.tokens;
-  r.tile = p.stacked ? c / per : batch;
+  r.tile = p.stacked ? (int)divide((uint32_t)c, a.by_rows) : batch;
   const int in = p.stacked ? c - r.tile * per : c;
-  const int g = in / a.tokens;
+  const int g = (int)divide((uint32_t)in, a.by_tokens);
   r.token = in - g * a.tokens;
   r.head = kvh * a.group + g;
   r.rid = (r.tile * a.kv_heads + kvh) * per + in;
@@ -192,7 +193,9 @@ __device__ __forceinline__ void ctx_finish(const CtxArgs& a, const CtxPart& p, u
 
 // ---------------------------------------------------------------------------------------------------- host side
 // The launches for at most kCtxTilesPerLaunch tiles and what they need of the workspace.
-enum { kCtxWide, kCtxSplit, kCtxSplit16 };   // workgroups of 128 rows that share their keys; wavefronts of 32 (fp32: or 16) rows with keys of their own
+constexpr int kCtxResidentBytes = 128 * 1024;
+enum { kCtxWide, kCtxSplit, kCtxSplit16, kCtxResident };   // workgroups of 128 rows that share their keys; wavefronts of 32 (fp32: or 16) rows with keys of their own;
+                                                         // bf16: all keys stay in LDS
 struct CtxPlan {
   int32_t n_launches;
   int32_t kind[2];
@@ -203,6 +206,7 @@ struct CtxPlan {
 };
 CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles);
 int launch_context_bf16_wide(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s);
+int launch_context_bf16_resident(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s);
 int launch_context_bf16_split(const CtxArgs& a, const CtxTable& tab, int head_dim, hipStream_t s);
 int launch_context_f32(const CtxArgs& a, const CtxTable& tab, int kind, int head_dim, hipStream_t s);
 int launch_context_join(const CtxArgs& a, const CtxTable& tab, int head_dim, int dtype, hipStream_t s);

@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const 
 #pragma unroll
       for (int jj = 0; jj < D / 16; ++jj) {
         const f32x4 x = *(const f32x4*)(src + 16 * jj + 4 * grp);
-        q[qb][jj] = row.there ? x * a.scale : f32x4{0.f, 0.f, 0.f, 0.f};
+        q[qb][jj] = x * a.scale;
       }
     }
     uint32_t kfrag[D / 16];   // offsets inside a half stage: row lq, chunk 4 jj + grp

@@ -67,8 +67,11 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
   const int keys = (bf16 ? 32 : 16) * (p.head_dim == 128 ? 1 : 2), wide_keys = bf16 ? 64 : keys;   // of a wavefront's, of a shared stage
   auto stages = [](int tokens, int of) -> int64_t { return (tokens + of - 1) / of; };
   const int tile_keys = prefix ? p.own_tokens : p.ctx_tokens, shared_keys = prefix ? p.ctx_tokens : 0;
-  // fp32, 16 rows per wavefront instead of 32: where there are no more, and where blocks of 32 leave compute units without work
-  auto split_kind = [&](int64_t batches, int64_t n) { return !bf16 && (n <= 16 || batches * p.kv_heads * ((n + 31) / 32) < kCus) ? kCtxSplit16 : kCtxSplit; };
+  // fp32, 16 rows per wavefront instead of 32: where there are no more, and where wavefronts of 32 would have less than four stages each (4 tiles
+  // of 300 queries, 2 heads x 64, over 377 keys: 17.6 -> 11.5 us; 64 rows over 16,000 keys, the other way round: 37 and 46 us)
+  auto split_kind = [&](int64_t batches, int64_t n, int64_t of) {
+    return !bf16 && (n <= 16 || batches * p.kv_heads * ((n + 31) / 32) * of < 16 * kCus) ? kCtxSplit16 : kCtxSplit;
+  };
   auto wave_rows = [](int kind) { return kind == kCtxSplit16 ? 16 : 32; };
   plan.n_launches = 1;
   CtxPart &first = plan.part[0], &second = plan.part[1];
@@ -80,13 +83,13 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
       plan.kind[0] = kCtxWide;
       cut_wide(first, 1, all, p.kv_heads, stages(shared_keys, wide_keys));
     } else {
-      plan.kind[0] = split_kind(1, all);
+      plan.kind[0] = split_kind(1, all, stages(shared_keys, keys));
       cut(first, 1, all, p.kv_heads, stages(shared_keys, keys), wave_rows(plan.kind[0]), 4 * kCus);
     }
     first.seg0 = first.stacked = 1;
     if (tile_keys > 0) {
       plan.n_launches = 2;
-      plan.kind[1] = split_kind(n_tiles, rows);
+      plan.kind[1] = split_kind(n_tiles, rows, stages(tile_keys, keys));
       cut(second, n_tiles, rows, p.kv_heads, stages(tile_keys, keys), wave_rows(plan.kind[1]), 4 * kCus);
       second.seg1 = 1;
       second.first_share = first.splits;
@@ -102,12 +105,19 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
     }
   } else {
     const int64_t blocks = (int64_t)n_tiles * p.kv_heads * ((rows + 127) / 128);
-    if (blocks >= kCus) {
+    const int64_t row_blocks = (rows + 31) / 32, units = stages(shared_keys, 64) + stages(tile_keys, 64);
+    if (bf16 && units * 64 * p.head_dim * 4 <= kCtxResidentBytes && n_tiles * p.kv_heads * row_blocks >= 16 * kCus &&
+        n_tiles * p.kv_heads * row_blocks < (1 << 30)) {
+      plan.kind[0] = kCtxResident;
+      first.rows = (int32_t)rows;
+      first.row_blocks = (int32_t)row_blocks;
+      first.splits = first.ways = first.items = 1;
+    } else if (blocks >= kCus) {
       plan.kind[0] = kCtxWide;
       cut_wide(first, n_tiles, rows, p.kv_heads, 1);
     } else {
-      plan.kind[0] = split_kind(n_tiles, rows);
       const int64_t n = stages(shared_keys, keys) + stages(tile_keys, keys);
+      plan.kind[0] = split_kind(n_tiles, rows, n);
       cut(first, n_tiles, rows, p.kv_heads, n > 0 ? n : 1, wave_rows(plan.kind[0]), 4 * kCus);
     }
     first.seg0 = prefix;
