@@ -44,11 +44,12 @@ void cut(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages, in
   const int64_t items = (int64_t)batches * kv_heads * p.row_blocks * p.splits;
   p.items = items > (1 << 30) ? -1 : (int32_t)items;
 }
-// The same for workgroups of 128 rows, of which there should be one for each compute unit.
+// The same for workgroups of 128 rows, of which there should be one for each compute unit (512 rows over a prefix of 16,384 keys, 8 heads x 128:
+// 47.6 us, with two for each 52.7), of at least eight stages (256 blocks of 32 rows x 128 over 500 keys: 14.5 us, with four 19.4).
 void cut_wide(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages) {
   const int64_t blocks = (rows + 127) / 128, base = batches * kv_heads * blocks;
   int64_t splits = kCus / base;
-  const int64_t most = stages / 4 > 1 ? stages / 4 : 1;   // at least four stages for a share
+  const int64_t most = stages / 8 > 1 ? stages / 8 : 1;
   splits = splits < 1 ? 1 : (splits > most ? most : splits);
   p.ways = 1;
   p.splits = (int32_t)splits;
@@ -105,16 +106,22 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
     }
   } else {
     const int64_t blocks = (int64_t)n_tiles * p.kv_heads * ((rows + 127) / 128);
-    const int64_t row_blocks = (rows + 31) / 32, units = stages(shared_keys, 64) + stages(tile_keys, 64);
-    if (bf16 && units * 64 * p.head_dim * 4 <= kCtxResidentBytes && n_tiles * p.kv_heads * row_blocks >= 16 * kCus &&
-        n_tiles * p.kv_heads * row_blocks < (1 << 30)) {
+    const int64_t row_blocks = (rows + 31) / 32, all = n_tiles * p.kv_heads * row_blocks;
+    const int64_t units = stages(shared_keys, 64) + stages(tile_keys, 64), wide_stages = stages(shared_keys, wide_keys) + stages(tile_keys, wide_keys);
+    // Keys that fit stay in LDS where its wavefronts, 8 for each compute unit, have two row blocks each: head_dim 64, 500 keys, 8,192 row blocks
+    // 47.4 us (shared stages: 54.8), 4,096 28.0 (30.0), 2,048 16.5 (16.4); head_dim 128, 250 keys 49.8 (59.5), 27.4 (31.5), 17.9 (17.6).
+    if (bf16 && units * 64 * p.head_dim * 4 <= kCtxResidentBytes && all >= 16 * kCus && all < (1 << 30)) {
       plan.kind[0] = kCtxResident;
       first.rows = (int32_t)rows;
       first.row_blocks = (int32_t)row_blocks;
       first.splits = first.ways = first.items = 1;
-    } else if (blocks >= kCus) {
+    } else if (blocks >= (bf16 ? kCus / 2 : kCus) || blocks * wide_stages * wide_keys * p.head_dim >= (bf16 ? 10 : 16) * kCus * 64 * 64) {
+      // Shared stages read a key from memory once for 128 rows, wavefronts with keys of their own once for 32, but those need no barriers and
+      // start and join sooner.  128 blocks of 128 rows, head_dim 128, 500 keys: 14.8 us (own keys: 19.1), 64 the same: 14.5 and 16.2, head_dim 64
+      // 11.6 and 10.7.  Fewer blocks over more keys: 16 blocks, 8,000 keys x 128 23.2 (30.6), 2,000 20.0 (15.8).
+      // fp32: 128 blocks, 500 keys x 128 61.4 us (51.9), 80 blocks, 2,000 keys x 128 119 (172), 24 blocks, 8,000 keys x 128 135 (124).
       plan.kind[0] = kCtxWide;
-      cut_wide(first, n_tiles, rows, p.kv_heads, 1);
+      cut_wide(first, n_tiles, rows, p.kv_heads, wide_stages > 0 ? wide_stages : 1);
     } else {
       const int64_t n = stages(shared_keys, keys) + stages(tile_keys, keys);
       plan.kind[0] = split_kind(n_tiles, rows, n);
