@@ -1,7 +1,8 @@
 // Residual addition and root-mean-square norm of the rows of tiles, in the tensors' type or in 8 bits with scales (sg_tile_residual_norm):
 //     s = x + r,   y = s * rsqrt(mean(s^2) + eps) * w,   out = y   or   out = e4m3(y * 448 / a), scale = a / 448, a = max|y| of a row or block
 // Everything between the loads and the stores is fp32 and stays in registers: one read of x and r, one write of s and out.  Bound by
-// memory.
+// memory: 75,600 rows of 5,120, bf16 + bf16 to bf16 and e4m3 437 us (6.2 TB/s; a large copy runs at 5.4), 9 tiles of 153,600 rows of 128 in bf16
+// 131 us (5.4 TB/s).
 //
 // Rows of up to 512 channels share a wavefront (the lanes of a row are a power of two), up to 2,048 take a wavefront each, up to 8,192 a
 // workgroup of 4 and beyond that one of 16 wavefronts, so that a lane never holds more than 4 vectors of 8 channels and enough
@@ -33,19 +34,23 @@ struct NormArgs {
   float eps;
 };
 
-template <typename T> struct Vec8;   // 8 channels as they are stored
+// 8 channels as they are stored.  Rows pass once and are not to stay in the caches (75,600 rows of 5,120, bf16 to e4m3: 454 -> 440 us; fp32, whose
+// 32 bytes a lane take two accesses that meet in the cache, loses by it: 276 -> 323 us at 4,096 channels).
+template <typename T> struct Vec8;
 template <> struct Vec8<uint16_t> {
   u32x4 w;
   __device__ __forceinline__ void load(const uint16_t* p) { w = *(const u32x4*)p; }
+  __device__ __forceinline__ void stream(const uint16_t* p) { w = __builtin_nontemporal_load((const u32x4*)p); }
   __device__ __forceinline__ float get(int i) const { return i & 1 ? __uint_as_float(w[i >> 1] & 0xffff0000u) : __uint_as_float(w[i >> 1] << 16); }
 };
 template <> struct Vec8<float> {
   f32x4 a, b;
   __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
+  __device__ __forceinline__ void stream(const float* p) { load(p); }
   __device__ __forceinline__ float get(int i) const { return i < 4 ? a[i] : b[i - 4]; }
 };
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
-  *(u32x4*)p = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  __builtin_nontemporal_store(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])}, (u32x4*)p);
 }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
@@ -102,8 +107,8 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel
 #pragma unroll
     for (int i = 0; i < VPL; ++i)
       if (there && first + i * lanes < a.n_vec) {
-        xv[i].load(x + 8 * (first + i * lanes));
-        if (a.has_residual) rv[i].load(r + 8 * (first + i * lanes));
+        xv[i].stream(x + 8 * (first + i * lanes));
+        if (a.has_residual) rv[i].stream(r + 8 * (first + i * lanes));
       }
     float s[VPL][8];
     float sq = 0.f;
@@ -170,7 +175,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel
         lo = __builtin_amdgcn_cvt_pk_fp8_f32(s[i][2] * inv, s[i][3] * inv, lo, true);
         hi = __builtin_amdgcn_cvt_pk_fp8_f32(s[i][4] * inv, s[i][5] * inv, hi, false);
         hi = __builtin_amdgcn_cvt_pk_fp8_f32(s[i][6] * inv, s[i][7] * inv, hi, true);
-        if (there && first + i * lanes < a.n_vec) *(u32x2*)(o + 8 * (first + i * lanes)) = u32x2{(uint32_t)lo, (uint32_t)hi};
+        if (there && first + i * lanes < a.n_vec) __builtin_nontemporal_store(u32x2{(uint32_t)lo, (uint32_t)hi}, (u32x2*)(o + 8 * (first + i * lanes)));
       }
     }
   }
@@ -227,7 +232,10 @@ int launch_residual_norm(const sg_norm_problem& p, int n_tiles, const void* cons
     a.n_rows = (int64_t)n * p.rows;
     a.run = run ? run + t0 : nullptr;
     int64_t grid = (a.n_rows + rows_per_wg - 1) / rows_per_wg;
-    const int64_t most = waves == 16 ? 512 : 2048;   // 32 wavefronts for each of 256 compute units walk the rows
+    // Workgroups that walk the rows load the weight once, new ones overlap their start with the others' end.  One per row of 4 wavefronts: 75,600 rows
+    // of 5,120 454 us (2,048 that walk them: 536).  A wavefront per row: 8,192 workgroups, 768 channels 336 -> 297 us.  Shorter rows and
+    // rows of 16 wavefronts fill the chip once and walk: 128 channels 136 us, with 8,192 workgroups 140 us; 30,720 303 us, with 2,048 319 us.
+    const int64_t most = waves == 16 ? 512 : waves == 4 ? 1 << 22 : a.lanes == 64 ? 8192 : 2048;
     if (grid > most) grid = most;
     int st;
     if (p.dtype == SG_F32) st = p.out_dtype == SG_F8_E4M3 ? launch<float, true>(a, tab, vpl, waves, grid, s) : launch<float, false>(a, tab, vpl, waves, grid, s);
