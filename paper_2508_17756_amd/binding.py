@@ -520,23 +520,29 @@ def _scratch(workspace):
     return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
 
 
-def _pointers(tensors):
-    """_ptr_array, or NULL for no list."""
-    return None if tensors is None else _ptr_array(tensors)
+def _pointers(tensors, n):
+    """_ptr_array of one tensor for each of n tiles, or NULL for no list."""
+    if tensors is None:
+        return None
+    if len(tensors) != n:
+        raise ValueError("%d tensors for %d tiles" % (len(tensors), n))
+    return _ptr_array(tensors)
 
 
 def sg_tile_cross_attention(p, q, k, v, out, ctx_len=None, key_mask=None, run=None, workspace=None):
     """q, k, v, out: lists of one tensor per tile (k, v: None if the context has no tokens); ctx_len: int32, key_mask and run: uint8."""
-    st = load_library().sg_tile_cross_attention(ctypes.byref(p), len(q), _ptr_array(q), _pointers(k), _pointers(v), _ptr(ctx_len),
-                                                _ptr(key_mask), _ptr(run), _ptr_array(out), *_scratch(workspace), _stream())
+    n = len(q)
+    st = load_library().sg_tile_cross_attention(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _pointers(v, n), _ptr(ctx_len),
+                                                _ptr(key_mask), _ptr(run), _pointers(out, n), *_scratch(workspace), _stream())
     _check(st, "sg_tile_cross_attention")
     return out
 
 
 def sg_tile_prefix_attention(p, q, k, v, prefix_k, prefix_v, out, own_len=None, prefix_len=None, run=None, workspace=None):
     """q, k, v, out: lists of one tensor per tile (k, v: None if tiles have no keys of their own); own_len, prefix_len: int32; run: uint8."""
-    st = load_library().sg_tile_prefix_attention(ctypes.byref(p), len(q), _ptr_array(q), _pointers(k), _pointers(v), _ptr(prefix_k),
-                                                 _ptr(prefix_v), _ptr(own_len), _ptr(prefix_len), _ptr(run), _ptr_array(out),
+    n = len(q)
+    st = load_library().sg_tile_prefix_attention(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _pointers(v, n), _ptr(prefix_k),
+                                                 _ptr(prefix_v), _ptr(own_len), _ptr(prefix_len), _ptr(run), _pointers(out, n),
                                                  *_scratch(workspace), _stream())
     _check(st, "sg_tile_prefix_attention")
     return out
@@ -551,7 +557,8 @@ def make_norm_problem(rows, channels, dtype, out_dtype=None, scale_group=0, eps=
 
 def sg_tile_residual_norm(p, x, weight, out, residual=None, sum_out=None, out_scale=None, run=None):
     """x, out, residual, sum_out, out_scale: lists of one tensor per tile, the last three or None; weight: `channels` elements or None."""
-    st = load_library().sg_tile_residual_norm(ctypes.byref(p), len(x), _ptr_array(x), _pointers(residual), _ptr(weight), _ptr(run),
-                                              _pointers(sum_out), _ptr_array(out), _pointers(out_scale), _stream())
+    n = len(x)
+    st = load_library().sg_tile_residual_norm(ctypes.byref(p), n, _ptr_array(x), _pointers(residual, n), _ptr(weight), _ptr(run),
+                                              _pointers(sum_out, n), _pointers(out, n), _pointers(out_scale, n), _stream())
     _check(st, "sg_tile_residual_norm")
     return out

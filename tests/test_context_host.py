@@ -40,6 +40,7 @@ def _problem(**fields):
     ({"head_dim": 128, "q_stride_token": 128, "ctx_stride_token": 128, "own_stride_token": 128, "out_stride_token": 128,
       "out_stride_head": 12 * 128}, sg.SG_OK),
     ({"head_dim": 32}, sg.SG_ERR_UNSUPPORTED), ({"ctx_stride_token": 1 << 22}, sg.SG_ERR_UNSUPPORTED),
+    ({"heads": 65536, "kv_heads": 65536, "tokens": 1}, sg.SG_ERR_UNSUPPORTED), ({"heads": 65536, "kv_heads": 32768, "tokens": 1}, sg.SG_OK),
     ({"own_stride_token": 1 << 22}, sg.SG_ERR_UNSUPPORTED), ({"tokens": 1 << 23, "out_stride_head": 64 << 23}, sg.SG_ERR_UNSUPPORTED),
 ])
 def test_context_problem_is_checked(fields, status):
@@ -141,3 +142,24 @@ def test_norm_calls_are_refused():
     for group, status in ((96, bad), (-128, bad), (64, sg.SG_ERR_UNSUPPORTED), (256, sg.SG_ERR_UNSUPPORTED)):
         p8.scale_group = group
         assert _norm(p8, scale=True) == status, group
+
+
+class _Host:
+    """A tensor's stand-in for the binding."""
+
+    def data_ptr(self):
+        return GOOD
+
+
+def test_lists_of_unequal_length_are_refused():
+    """The library reads one pointer per tile from each list."""
+    p, two, one = _problem(), [_Host()] * 2, [_Host()]
+    for k, v, out in ((one, two, two), (two, one, two), (two, two, one), (two, two, two + one)):
+        with pytest.raises(ValueError):
+            sg.sg_tile_cross_attention(p, two, k, v, out)
+        with pytest.raises(ValueError):
+            sg.sg_tile_prefix_attention(p, two, k, v, _Host(), _Host(), out)
+    n = sg.make_norm_problem(5, 256, "bf16")
+    for lists in ({"out": one}, {"residual": one}, {"sum_out": one}, {"out_scale": one}):
+        with pytest.raises(ValueError):
+            sg.sg_tile_residual_norm(n, two, None, **{"out": two, **lists})

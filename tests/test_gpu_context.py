@@ -47,6 +47,47 @@ def test_cross_many_rows(d, lay, tiles, tokens, heads, kv_heads, ctx):
     c.check(c.out, before, heads=[0, 1, heads // 2, heads - 1])
 
 
+# more row blocks than the wavefronts that keep a head's keys in LDS take at once (two for each of 256 x 8): the most keys that fit, one, none;
+# grouped heads, ranges of row blocks that pass from head to head and from tile to tile
+@pytest.mark.parametrize("lay", ["packed", "token", "odd"])
+@pytest.mark.parametrize("d, tiles, tokens, heads, kv_heads, ctx", [(64, 4, 540, 64, 64, 512), (128, 4, 540, 64, 64, 256), (64, 3, 2100, 24, 24, 226),
+                                                                    (128, 3, 2100, 24, 24, 77), (64, 5, 300, 128, 32, 130), (64, 65, 33, 64, 32, 40),
+                                                                    (128, 2, 33, 1024, 1024, 1)])
+def test_cross_over_few_keys(lay, d, tiles, tokens, heads, kv_heads, ctx):
+    c = Call(tiles, tokens, heads, kv_heads, d, "bf16", ctx, lay=lay, ragged=True, masked=ctx > 1, run=tiles > 2, seed=ctx)
+    before = [t.clone() for t in c.out]
+    c()
+    torch.cuda.synchronize()
+    c.check(c.out, before, heads=[0, 1, heads // 2, heads - 1])
+
+
+@pytest.mark.parametrize("lay", ["packed", "odd"])
+@pytest.mark.parametrize("d, own, prefix", [(64, 130, 300), (128, 60, 190), (64, 1, 1), (64, 0, 512), (128, 256, 0)])
+def test_prefix_and_own_keys_that_fit(lay, d, own, prefix):
+    for length in (None, 0, prefix // 2):
+        c = Call(4, 540, 64, 64, d, "bf16", prefix, own=own, prefix=True, lay=lay, ragged=own > 0, run=True, seed=own)
+        c.prefix_len = None if length is None else torch.tensor([length], dtype=torch.int32)
+        before = [t.clone() for t in c.out]
+        c()
+        torch.cuda.synchronize()
+        c.check(c.out, before, heads=[0, 31, 63])
+
+
+# few blocks of 128 rows over many keys, shared and cut into shares, which a second launch joins
+@pytest.mark.parametrize("dtype, d, tiles, tokens, heads, kv_heads, ctx", [
+    ("bf16", 128, 1, 1000, 2, 2, 8000), ("bf16", 64, 2, 500, 16, 8, 2001), ("bf16", 128, 3, 129, 8, 4, 1500), ("f32", 128, 2, 300, 8, 8, 1999),
+    ("f32", 64, 1, 600, 16, 16, 2500)])
+@pytest.mark.parametrize("lay", ["packed", "odd"])
+def test_cross_of_many_rows_and_keys(dtype, d, tiles, tokens, heads, kv_heads, ctx, lay):
+    for prefix in (False, True):
+        c = Call(tiles, tokens, heads, kv_heads, d, dtype, 500 if prefix else ctx, own=ctx - 500 if prefix else 0, prefix=prefix, lay=lay,
+                 ragged=tiles > 1, masked=not prefix, run=tiles > 2, seed=ctx)
+        before = [t.clone() for t in c.out]
+        c()
+        torch.cuda.synchronize()
+        c.check(c.out, before, heads=[0, heads - 1])
+
+
 @pytest.mark.parametrize("dtype", DT)
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("tiles, tokens, heads, kv_heads, own, prefix", [
@@ -272,3 +313,106 @@ def test_refused_on_the_device_side_too():
         sg.sg_tile_prefix_attention(c.p, c.q, c.k, c.v, c.pk, c.pv, c.out)      # no workspace
     with pytest.raises(sg.SgError):
         sg.sg_tile_prefix_attention(c.p, c.q, c.k, c.v, c.pk, None, c.out, workspace=c.workspace())
+
+
+@pytest.mark.parametrize("d, ctx", [(64, 500), (128, 250)])
+@pytest.mark.parametrize("poison", [float("nan"), float("inf"), -3.0e38])
+def test_what_does_not_count_is_not_read_into_lds(d, ctx, poison):
+    c = Call(4, 540, 64, 64, d, "bf16", ctx, ragged=True, masked=True, seed=3)
+    c.lens = torch.tensor([ctx - 1, 70, 0, ctx], dtype=torch.int32)
+    c.mask[0, :64] = 0
+    clean = [[t.clone() for t in ts] for ts in (c.k, c.v)]
+    for i in range(4):
+        drop = torch.ones(ctx, dtype=torch.bool)
+        drop[c.keys(i)] = False
+        c.k[i][:, drop.to("cuda")] = poison
+        c.v[i][:, drop.to("cuda")] = poison
+    out = [t.clone() for t in c()]
+    c.k, c.v = clean
+    c.check(out, heads=[0, 33])
+    # a NaN that counts, in one channel of a head of the first tile
+    at = int(c.keys(0)[5])
+    c.v[0][7, at, 3] = float("nan")
+    c.q[1][9, 11, 0] = float("nan")
+    out = c()
+    torch.cuda.synchronize()
+    for i in range(4):
+        want = torch.zeros(out[i].shape, dtype=torch.bool)
+        if i == 0:
+            want[7, :, 3] = True
+        if i == 1:
+            want[9, 11, :] = True
+        assert torch.equal(torch.isnan(out[i].cpu()), want)
+
+
+@pytest.mark.parametrize("d, ctx", [(64, 512), (128, 256)])
+def test_rising_maxima_over_few_keys(d, ctx):
+    c = Call(1, 2100, 64, 64, d, "bf16", ctx, spread=8.0, seed=11)
+    c.k[0] *= torch.linspace(0.05, 1.0, ctx, device="cuda").to(c.k[0].dtype)[None, :, None]
+    c()
+    torch.cuda.synchronize()
+    c.check(heads=[0, 63])
+
+
+@pytest.mark.parametrize("tokens, heads, ctx", [(2100, 64, 300), (1000, 2, 6000)])
+def test_replays_of_cross_attention_with_changing_flags(tokens, heads, ctx):
+    """Lengths, masks and run flags are read by every replay; rows of a tile that does not run stay."""
+    c = Call(2, tokens, heads, heads, 64, "bf16", ctx, seed=6)
+    lens = torch.full((2,), ctx, dtype=torch.int32, device="cuda")
+    mask = torch.ones((2, ctx), dtype=torch.uint8, device="cuda")
+    run = torch.ones((2,), dtype=torch.uint8, device="cuda")
+    ws = c.workspace()
+    eager, graphed = [torch.zeros_like(t) for t in c.out], [torch.zeros_like(t) for t in c.out]
+
+    def call(out):
+        sg.sg_tile_cross_attention(c.p, c.q, c.k, c.v, out, ctx_len=lens, key_mask=mask, run=run, workspace=ws)
+
+    call(eager)
+    torch.cuda.synchronize()
+    g, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=side):
+        call(graphed)
+    torch.cuda.synchronize()
+    g.replay()
+    for k in range(4):
+        lens.copy_(torch.tensor([ctx - 31 * k, 100 * k], dtype=torch.int32))
+        mask[:, k::7] = 0
+        run[k & 1] = k < 2
+        c.q[0].mul_(0.9)
+        call(eager)
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(eager, graphed):
+            assert torch.equal(x, y)
+
+
+def test_two_calls_at_once_of_every_kind():
+    """Calls of different shapes on two streams, a workspace each, give what they give alone."""
+    calls = [Call(4, 540, 64, 64, 64, "bf16", 300, seed=1), Call(1, 1000, 4, 4, 128, "bf16", 4000, seed=2),
+             Call(20, 1, 8, 2, 128, "bf16", 3000, own=40, prefix=True, seed=3), Call(2, 300, 8, 8, 128, "f32", 1500, seed=4)]
+    want = [[t.clone() for t in c()] for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[[torch.zeros_like(t) for t in c.out] for c in calls] for _ in streams]
+    spaces = [[c.workspace() for c in calls] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for turn in range(len(calls)):
+            for i, s in enumerate(streams):
+                at = (turn + i) % len(calls)
+                with torch.cuda.stream(s):
+                    calls[at](workspace=spaces[i][at], out=got[i][at])
+    torch.cuda.synchronize()
+    for outs in got:
+        for o, w in zip(outs, want):
+            for x, y in zip(o, w):
+                assert torch.equal(x, y)
+
+
+def test_the_same_buffers_for_every_tile():
+    """Tiles may name the same context, and the same queries."""
+    c = Call(5, 40, 8, 2, 128, "bf16", 200, ragged=True, seed=5)
+    c.q, c.k, c.v = [c.q[0]] * 5, [c.k[0]] * 5, [c.v[0]] * 5
+    c.lens = torch.tensor([200, 0, 3, 64, 65], dtype=torch.int32)
+    _run(c)
