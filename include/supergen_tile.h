@@ -13,6 +13,8 @@
  *                           input (Equation 3) against a threshold (Equation 7)
  *   sg_denoise_step_tiled   one stage-2 step: gate -> attention on the tiles to recompute ->
  *                           cache refresh -> Fuse (Algorithm 1 loop body; Section 5.1 pipeline)
+ *   sg_tile_cross_attention, sg_tile_prefix_attention, sg_tile_residual_norm
+ *                           what the transformer block of a tile has beside its self-attention
  *
  * Conventions shared by every entry point
  *   - "device" pointers are HIP device memory on the current device; "host" pointers are
@@ -440,7 +442,8 @@ int sg_refine_step_canvas(const sg_problem* p, const void* q, const void* k, con
  *     base + a*stride_head + n*stride_token + c      (in elements)
  * so that [heads][tokens][d] and [tokens][heads][d] (what a projection leaves) are both expressible.  Keys and values of one
  * segment share their strides (those of a segment of 0 tokens are not looked at).  All strides are positive multiples of 8,
- * stride_token >= head_dim and below 2^22 for keys; heads * tokens is below 2^25; base pointers are 16-byte aligned. */
+ * stride_token >= head_dim and below 2^22 for keys; heads * tokens is below 2^25, kv_heads at most 65,535, each segment below
+ * 2^30 tokens; base pointers are 16-byte aligned. */
 typedef struct sg_context_problem {
   int32_t heads, kv_heads;    /* heads of the queries; of keys and values: a divisor of heads (head a reads a / (heads / kv_heads)) */
   int32_t head_dim;           /* 64 or 128                                                                       */
@@ -476,8 +479,10 @@ int sg_context_workspace_bytes(const sg_context_problem* p, int32_t n_tiles, siz
  *   run        device, n_tiles bytes (sg_cache_gate's recompute), or NULL: all tiles
  * bf16 problems multiply in bf16 on the matrix cores (probabilities are rounded to bf16 for the second product), accumulate
  * in fp32 and scale the scores in fp32 behind the product; f32 problems multiply and accumulate in fp32.  A NaN in Q, or at a
- * place that counts in K or V, reaches every output that depends on it, and no other.  Tiles are attended up to 64 a launch; calls with
- * few queries are cut along the keys and joined by a second launch.  The same call gives the same bits every time.
+ * place that counts in K or V, reaches every output that depends on it, and no other.  The exponentials' reference follows the
+ * largest score to within 2^5, so that sums of p v stay finite where 32 * keys * |v| does.  Tiles are attended up to 64 a launch; calls
+ * whose queries do not fill the device are cut along the keys and joined by a second launch.  The same call gives the same bits
+ * every time; a call of other sizes, or of more tiles, may be cut in another way and round differently.
  */
 int sg_tile_cross_attention(const sg_context_problem* p, int32_t n_tiles, const void* const* q, const void* const* k,
                             const void* const* v, const int32_t* ctx_len, const uint8_t* key_mask, const uint8_t* run,
@@ -492,8 +497,8 @@ int sg_tile_cross_attention(const sg_context_problem* p, int32_t n_tiles, const 
  *   prefix_k, prefix_v  device; with ctx_tokens = 0 not looked at
  *   k, v                host arrays of n_tiles device pointers; with own_tokens = 0 not looked at
  *   own_len             device, n_tiles lengths, or NULL: own_tokens each;  prefix_len: device, one length, or NULL: ctx_tokens
- * Everything else as sg_tile_cross_attention.  Where a tile has at most 16 queries per head of keys, those of all tiles (of a launch)
- * are stacked and the prefix is read once for all of them.
+ * Everything else as sg_tile_cross_attention.  Where a tile has at most 16 queries per head of keys
+ * and the prefix's buffers hold at least 128, those of all tiles (of a launch) are stacked and the prefix is read once for all of them.
  */
 int sg_tile_prefix_attention(const sg_context_problem* p, int32_t n_tiles, const void* const* q, const void* const* k,
                              const void* const* v, const void* prefix_k, const void* prefix_v, const int32_t* own_len,

@@ -10,6 +10,9 @@
 // Two forms.  Shared: the 4 wavefronts of a workgroup take rows of their own against the same stages of keys, for calls with rows to fill the
 // chip.  Otherwise every wavefront streams keys of its own through LDS of its own; wavefronts of a workgroup take other row blocks or other
 // shares of the keys, whichever there are more of (context_common.h).
+//
+// Bound by the fp32 matrix instruction where there are rows (4 tiles of 2,880, 8 heads x 128, 226 keys: 119 us, 89 TFLOP/s; a large product of
+// the library 154), by latency where there are few (4 tiles of 300, 2 heads x 64, 377 keys: 10.4 us).
 #include <atomic>
 #include "context_common.h"
 
