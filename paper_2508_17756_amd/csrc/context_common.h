@@ -194,7 +194,7 @@ __device__ __forceinline__ void ctx_finish(const CtxArgs& a, const CtxPart& p, u
 // ---------------------------------------------------------------------------------------------------- host side
 // The launches for at most kCtxTilesPerLaunch tiles and what they need of the workspace.
 constexpr int kCtxResidentBytes = 128 * 1024;
-enum { kCtxWide, kCtxSplit, kCtxSplit16, kCtxResident };   // workgroups of 128 rows that share their keys; wavefronts of 32 (fp32: or 16) rows with keys of their own;
+enum { kCtxWide, kCtxSplit, kCtxSplit16, kCtxResident };   // workgroups of 128 (fp32: 64) rows that share their keys; wavefronts of 32 (fp32: or 16) rows with keys of their own;
                                                          // bf16: all keys stay in LDS
 struct CtxPlan {
   int32_t n_launches;

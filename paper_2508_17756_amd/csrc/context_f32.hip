@@ -7,11 +7,11 @@
 // Row i of block db of O^T is channel 64 (db / 4) + 4 i + db % 4, so that a lane reads its values of four blocks, and writes its results, 16
 // bytes at a time.
 //
-// Two forms.  Shared: the 4 wavefronts of a workgroup take rows of their own against the same stages of keys, for calls with rows to fill the
-// chip.  Otherwise every wavefront streams keys of its own through LDS of its own; wavefronts of a workgroup take other row blocks or other
+// Two forms.  Shared: the 4 wavefronts of a workgroup take 16 rows each against the same stages of keys, for calls with rows to fill the
+// chip (32 each read fewer fragments, which do not bind, and end less evenly: 116 us for the 110 below).  Otherwise every wavefront streams keys of its own through LDS of its own; wavefronts of a workgroup take other row blocks or other
 // shares of the keys, whichever there are more of (context_common.h).
 //
-// Bound by the fp32 matrix instruction where there are rows (4 tiles of 2,880, 8 heads x 128, 226 keys: 119 us, 89 TFLOP/s; a large product of
+// Bound by the fp32 matrix instruction where there are rows (4 tiles of 2,880, 8 heads x 128, 226 keys: 110 us, 97 TFLOP/s; a large product of
 // the library 154), by latency where there are few (4 tiles of 300, 2 heads x 64, 377 keys: 10.4 us).
 #include <atomic>
 #include "context_common.h"
@@ -60,7 +60,7 @@ __device__ __forceinline__ float group_sum(float x) {
 }
 
 template <int D, int QB, bool SHARED>
-__global__ __launch_bounds__(256, SHARED ? 2 : 1) void context_f32_kernel(const CtxArgs a, const CtxTable tab) {
+__global__ __launch_bounds__(256, SHARED ? 3 : 1) void context_f32_kernel(const CtxArgs a, const CtxTable tab) {
   constexpr int kKeys = kHalfStage / (D * 4);   // 16 (head_dim 64: 32)
   constexpr int kBlocks = kKeys / 16;
   constexpr int kChunks = D / 4;                // 16-byte chunks of a row
@@ -321,7 +321,7 @@ int launch_context_f32(const CtxArgs& a, const CtxTable& tab, int kind, int head
     return SG_OK;
   };
   if (kind == kCtxWide)
-    return head_dim == 128 ? launch(context_f32_kernel<128, 2, true>, 4, kWaveLds) : launch(context_f32_kernel<64, 2, true>, 5, kWaveLds);
+    return head_dim == 128 ? launch(context_f32_kernel<128, 1, true>, 4, kWaveLds) : launch(context_f32_kernel<64, 1, true>, 5, kWaveLds);
   if (kind == kCtxSplit16)
     return head_dim == 128 ? launch(context_f32_kernel<128, 1, false>, 0, kLds) : launch(context_f32_kernel<64, 1, false>, 1, kLds);
   return head_dim == 128 ? launch(context_f32_kernel<128, 2, false>, 2, kLds) : launch(context_f32_kernel<64, 2, false>, 3, kLds);

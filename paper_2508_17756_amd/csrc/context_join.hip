@@ -44,11 +44,13 @@ void cut(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages, in
   const int64_t items = (int64_t)batches * kv_heads * p.row_blocks * p.splits;
   p.items = items > (1 << 30) ? -1 : (int32_t)items;
 }
-// The same for workgroups of 128 rows, of which there should be one for each compute unit (512 rows over a prefix of 16,384 keys, 8 heads x 128:
-// 47.6 us, with two for each 52.7), of at least eight stages (256 blocks of 32 rows x 128 over 500 keys: 14.5 us, with four 19.4).
-void cut_wide(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages) {
-  const int64_t blocks = (rows + 127) / 128, base = batches * kv_heads * blocks;
-  int64_t splits = kCus / base;
+// The same for workgroups that share stages of keys: of 128 rows in bf16, of which there should be one for each compute unit (100 rows over a prefix of
+// 32,760 keys, 8 heads x 128: 47.6 us, with two for each 52.7), of 64 in fp32, two for each (16 x 600 rows x 128 over 2,000 keys 110 us; 128 rows
+// and one for each 119, 64 and three 118); of at least eight stages (bf16, 64 blocks x 128 over 500 keys: 14.5 us, with four 19.4).
+int64_t shared_rows(bool bf16) { return bf16 ? 128 : 64; }
+void cut_wide(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages, bool bf16) {
+  const int64_t of = shared_rows(bf16), blocks = (rows + of - 1) / of, base = batches * kv_heads * blocks;
+  int64_t splits = (bf16 ? kCus : 2 * kCus) / base;
   const int64_t most = stages / 8 > 1 ? stages / 8 : 1;
   splits = splits < 1 ? 1 : (splits > most ? most : splits);
   p.ways = 1;
@@ -82,7 +84,7 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
     const int64_t all = n_tiles * rows;
     if (all > 64) {
       plan.kind[0] = kCtxWide;
-      cut_wide(first, 1, all, p.kv_heads, stages(shared_keys, wide_keys));
+      cut_wide(first, 1, all, p.kv_heads, stages(shared_keys, wide_keys), bf16);
     } else {
       plan.kind[0] = split_kind(1, all, stages(shared_keys, keys));
       cut(first, 1, all, p.kv_heads, stages(shared_keys, keys), wave_rows(plan.kind[0]), 4 * kCus);
@@ -105,7 +107,7 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
       plan.join = true;
     }
   } else {
-    const int64_t blocks = (int64_t)n_tiles * p.kv_heads * ((rows + 127) / 128);
+    const int64_t of = shared_rows(bf16), blocks = (int64_t)n_tiles * p.kv_heads * ((rows + of - 1) / of);
     const int64_t row_blocks = (rows + 31) / 32, all = n_tiles * p.kv_heads * row_blocks;
     const int64_t units = stages(shared_keys, 64) + stages(tile_keys, 64), wide_stages = stages(shared_keys, wide_keys) + stages(tile_keys, wide_keys);
     // Keys that fit stay in LDS where its wavefronts, 8 for each compute unit, have two row blocks each: head_dim 64, 500 keys, 8,192 row blocks
@@ -115,13 +117,14 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
       first.rows = (int32_t)rows;
       first.row_blocks = (int32_t)row_blocks;
       first.splits = first.ways = first.items = 1;
-    } else if (blocks >= (bf16 ? kCus / 2 : kCus) || blocks * wide_stages * wide_keys * p.head_dim >= (bf16 ? 10 : 16) * kCus * 64 * 64) {
-      // Shared stages read a key from memory once for 128 rows, wavefronts with keys of their own once for 32, but those need no barriers and
+    } else if (blocks >= (bf16 ? kCus / 2 : 2 * kCus) || blocks * wide_stages * wide_keys * p.head_dim >= (bf16 ? 10 : 9) * kCus * 64 * 64) {
+      // Shared stages read a key from memory once for 128 rows (fp32: 64), wavefronts with keys of their own once for 32, but those need no barriers and
       // start and join sooner.  128 blocks of 128 rows, head_dim 128, 500 keys: 14.8 us (own keys: 19.1), 64 the same: 14.5 and 16.2, head_dim 64
       // 11.6 and 10.7.  Fewer blocks over more keys: 16 blocks, 8,000 keys x 128 23.2 (30.6), 2,000 20.0 (15.8).
-      // fp32: 128 blocks, 500 keys x 128 61.4 us (51.9), 80 blocks, 2,000 keys x 128 119 (172), 24 blocks, 8,000 keys x 128 135 (124).
+      // fp32, blocks of 64 rows: 512 blocks, 500 keys x 128 80.7 us (95.5), 256 the same 56.2 (52.0); 80 blocks, 2,000 keys x 64 36.7 (47.5), 40 the same 30.6
+      // (27.1).
       plan.kind[0] = kCtxWide;
-      cut_wide(first, n_tiles, rows, p.kv_heads, wide_stages > 0 ? wide_stages : 1);
+      cut_wide(first, n_tiles, rows, p.kv_heads, wide_stages > 0 ? wide_stages : 1, bf16);
     } else {
       const int64_t n = stages(shared_keys, keys) + stages(tile_keys, keys);
       plan.kind[0] = split_kind(n_tiles, rows, n);
