@@ -21,14 +21,16 @@ constexpr int kWideSlots = D == 128 ? 64 : 32;
 template <int D>
 constexpr int kWideHalf = kWideSlots<D> * kSlot;   // keys (or values) of a stage
 template <int D>
-constexpr int kWideLds = 4 * kWideHalf<D>;         // two stages of keys, two of values
+constexpr int kWideLds = 4 * kWideHalf<D>;         // two stages of keys, two of values: of a group of 4 wavefronts
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs a, const CtxTable tab) {
+// WAYS groups of 4 wavefronts take the same rows and shares of the keys, each with LDS of its own.
+template <int D, int WAYS>
+__global__ __launch_bounds__(256 * WAYS, 2) void context_bf16_wide_kernel(const CtxArgs a, const CtxTable tab) {
   constexpr int kKeys = 64, kInstr = kWideSlots<D> / 16, kHalf = kWideHalf<D>;
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) & 3;
+  const int way = WAYS == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
+  const uint32_t lds_all = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem, lds0 = lds_all + way * kWideLds<D>;
   const int lq = lane & 31, half = lane >> 5;
   const CtxPart& p = a.part;
   // Only the tiles that run are numbered, so that the work is spread evenly whichever they are.
@@ -45,7 +47,8 @@ __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs
 
   const Segment g0 = segment(a, tab, 0, tile, kvh), g1 = segment(a, tab, 1, tile, kvh);
   const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
-  const int from = (int)((int64_t)(n0 + n1) * split / p.splits), n = (int)((int64_t)(n0 + n1) * (split + 1) / p.splits) - from;   // stages: j = 0 is `from`
+  const int part = split * WAYS + way, parts = p.splits * WAYS;
+  const int from = (int)((int64_t)(n0 + n1) * part / parts), n = (int)((int64_t)(n0 + n1) * (part + 1) / parts) - from;   // stages: j = 0 is `from`
 
   bool mask_next = true;   // of the stage whose keys are requested next: whether key key0 + lane is unmasked
   auto fetch_mask = [&](int j) SG_INLINE {
@@ -252,6 +255,37 @@ __global__ __launch_bounds__(256, 2) void context_bf16_wide_kernel(const CtxArgs
   const uint32_t lu = __float_as_uint(l);
   const auto sw = __builtin_amdgcn_permlane32_swap(lu, lu, false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if constexpr (WAYS == 2) {
+    // The second group passes its share on through LDS, a register of all lanes behind another: sums where its stages were, (reference, sum) where
+    // the first group's were.
+    const int other = way == 0 ? 1 : 0, there = (int)((int64_t)(n0 + n1) * (split * 2 + other + 1) / parts) - (int)((int64_t)(n0 + n1) * (split * 2 + other) / parts);
+    for (int i = n > 0 ? n + 2 : 0; i < (there > 0 ? there + 2 : 0); ++i) meet();   // the other group's barriers
+    meet();
+    const uint32_t sums = lds_all + kWideLds<D> + (wave * 64 + lane) * 16, ml = lds_all + (wave * 64 + lane) * 8;
+    if (way == 1) {
+      *(SG_LDS f32x2*)(uintptr_t)ml = f32x2{m, l};
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *(SG_LDS f32x4*)(uintptr_t)(sums + (4 * db + g) * 4096) = f32x4{o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]};
+    }
+    __syncthreads();
+    if (way == 1) return;
+    const f32x2 x = *(const SG_LDS f32x2*)(uintptr_t)ml;
+    const float top = fmaxf(m, x[0]);
+    const float e0 = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - top), e1 = x[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[0] - top);   // 0: no keys
+    m = top;
+    l = l * e0 + x[1] * e1;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 v = *(const SG_LDS f32x4*)(uintptr_t)(sums + (4 * db + g) * 4096);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[db][4 * g + e] = o[db][4 * g + e] * e0 + v[e] * e1;
+      }
+  }
   const CtxRow mine = ctx_row(a, p, tile, kvh, row0 + lq);
   if (a.n_shares > 0) {   // a share: sums and reference for the join
     if (!mine.there) return;
@@ -274,7 +308,7 @@ int launch_context_bf16_wide(const CtxArgs& a, const CtxTable& tab, int head_dim
   int dev = 0;
   SG_HIP_TRY(hipGetDevice(&dev));
   constexpr int kMaxDevices = 64;
-  static std::atomic<bool> attr_set[kMaxDevices][2];   // the kernels' dynamic-LDS limit has been raised
+  static std::atomic<bool> attr_set[kMaxDevices][3];   // the kernels' dynamic-LDS limit has been raised
   auto launch = [&](auto kern, int slot, int lds) -> int {
     const int64_t grid = ((int64_t)a.part.items + 7) / 8 * 8;
     if (grid == 0) return SG_OK;
@@ -282,11 +316,12 @@ int launch_context_bf16_wide(const CtxArgs& a, const CtxTable& tab, int head_dim
       SG_HIP_TRY(hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
       if (dev >= 0 && dev < kMaxDevices) attr_set[dev][slot].store(true, std::memory_order_release);
     }
-    kern<<<dim3((unsigned)grid), 256, lds, s>>>(a, tab);
+    kern<<<dim3((unsigned)grid), 256 * a.part.ways, lds, s>>>(a, tab);
     SG_HIP_TRY(hipGetLastError());
     return SG_OK;
   };
-  return head_dim == 128 ? launch(context_bf16_wide_kernel<128>, 0, kWideLds<128>) : launch(context_bf16_wide_kernel<64>, 1, kWideLds<64>);
+  if (a.part.ways == 2) return launch(context_bf16_wide_kernel<64, 2>, 2, 2 * kWideLds<64>);   // (head_dim 64 alone: plan_context)
+  return head_dim == 128 ? launch(context_bf16_wide_kernel<128, 1>, 0, kWideLds<128>) : launch(context_bf16_wide_kernel<64, 1>, 1, kWideLds<64>);
 }
 
 }  // namespace sg

@@ -48,12 +48,15 @@ void cut(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages, in
 // 32,760 keys, 8 heads x 128: 47.6 us, with two for each 52.7), of 64 in fp32, two for each (16 x 600 rows x 128 over 2,000 keys 110 us; 128 rows
 // and one for each 119, 64 and three 118); of at least eight stages (bf16, 64 blocks x 128 over 500 keys: 14.5 us, with four 19.4).
 int64_t shared_rows(bool bf16) { return bf16 ? 128 : 64; }
-void cut_wide(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages, bool bf16) {
+void cut_wide(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stages, bool bf16, int head_dim) {
   const int64_t of = shared_rows(bf16), blocks = (rows + of - 1) / of, base = batches * kv_heads * blocks;
   int64_t splits = (bf16 ? kCus : 2 * kCus) / base;
   const int64_t most = stages / 8 > 1 ? stages / 8 : 1;
   splits = splits < 1 ? 1 : (splits > most ? most : splits);
-  p.ways = 1;
+  // head_dim 64: two groups of wavefronts share a workgroup's keys where it has its compute unit alone and eight stages (256 blocks over 2,000 keys
+  // 33.4 -> 27.1 us, over 500 12.2 -> 11.5, over 77 7.2 and 7.6; head_dim 128, whose stages are bound by more than one wavefront's chain, 42.4 and 40.5,
+  // 16.0 and 16.4)
+  p.ways = bf16 && head_dim == 64 && base * splits <= kCus && stages / splits >= 8 ? 2 : 1;
   p.splits = (int32_t)splits;
   p.rows = (int32_t)rows;
   p.row_blocks = (int32_t)blocks;
@@ -84,7 +87,7 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
     const int64_t all = n_tiles * rows;
     if (all > 64) {
       plan.kind[0] = kCtxWide;
-      cut_wide(first, 1, all, p.kv_heads, stages(shared_keys, wide_keys), bf16);
+      cut_wide(first, 1, all, p.kv_heads, stages(shared_keys, wide_keys), bf16, p.head_dim);
     } else {
       plan.kind[0] = split_kind(1, all, stages(shared_keys, keys));
       cut(first, 1, all, p.kv_heads, stages(shared_keys, keys), wave_rows(plan.kind[0]), 4 * kCus);
@@ -124,7 +127,7 @@ CtxPlan plan_context(const sg_context_problem& p, bool prefix, int n_tiles) {
       // fp32, blocks of 64 rows: 512 blocks, 500 keys x 128 80.7 us (95.5), 256 the same 56.2 (52.0); 80 blocks, 2,000 keys x 64 36.7 (47.5), 40 the same 30.6
       // (27.1).
       plan.kind[0] = kCtxWide;
-      cut_wide(first, n_tiles, rows, p.kv_heads, wide_stages > 0 ? wide_stages : 1, bf16);
+      cut_wide(first, n_tiles, rows, p.kv_heads, wide_stages > 0 ? wide_stages : 1, bf16, p.head_dim);
     } else {
       const int64_t n = stages(shared_keys, keys) + stages(tile_keys, keys);
       plan.kind[0] = split_kind(n_tiles, rows, n);

@@ -76,7 +76,7 @@ def test_prefix_and_own_keys_that_fit(lay, d, own, prefix):
 # few blocks of 128 rows over many keys, shared and cut into shares, which a second launch joins
 @pytest.mark.parametrize("dtype, d, tiles, tokens, heads, kv_heads, ctx", [
     ("bf16", 128, 1, 1000, 2, 2, 8000), ("bf16", 64, 2, 500, 16, 8, 2001), ("bf16", 128, 3, 129, 8, 4, 1500), ("f32", 128, 2, 300, 8, 8, 1999),
-    ("f32", 64, 1, 600, 16, 16, 2500)])
+    ("f32", 64, 1, 600, 16, 16, 2500), ("bf16", 64, 3, 400, 25, 25, 1031), ("bf16", 64, 1, 1000, 8, 4, 8003)])
 @pytest.mark.parametrize("lay", ["packed", "odd"])
 def test_cross_of_many_rows_and_keys(dtype, d, tiles, tokens, heads, kv_heads, ctx, lay):
     for prefix in (False, True):
@@ -416,3 +416,15 @@ def test_the_same_buffers_for_every_tile():
     c.q, c.k, c.v = [c.q[0]] * 5, [c.k[0]] * 5, [c.v[0]] * 5
     c.lens = torch.tensor([200, 0, 3, 64, 65], dtype=torch.int32)
     _run(c)
+
+
+@pytest.mark.parametrize("lens", [[577, 0, 1, 64], [65, 128, 129, 1]])
+def test_two_groups_of_a_workgroup_with_unequal_shares(lens):
+    """Tiles whose keys fill no stage, one, an odd number of them: one group of wavefronts may have nothing."""
+    c = Call(4, 500, 16, 16, 64, "bf16", 577, masked=True, seed=2)
+    c.lens = torch.tensor(lens, dtype=torch.int32)
+    c.mask[0, :512] = 0
+    c.mask[3] = 1
+    c()
+    torch.cuda.synchronize()
+    c.check(heads=[0, 15])
