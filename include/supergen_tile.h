@@ -463,7 +463,8 @@ int sg_context_validate(const sg_context_problem* p);
 
 /* Bytes of device scratch that the two calls below need for n_tiles tiles (the larger of the two; it may be 0).  The
  * workspace is 256-byte aligned device memory; it needs no initialisation and may be reused by the next call on the same
- * stream.  Two calls that may run at the same time (streams, graphs) need a workspace each. */
+ * stream.  Two calls that may run at the same time (streams, graphs) need a workspace each.  Fewer tiles can need more (their keys
+ * are cut further): a workspace for several tile counts has the largest of their sizes. */
 int sg_context_workspace_bytes(const sg_context_problem* p, int32_t n_tiles, size_t* out_bytes);
 
 /*
