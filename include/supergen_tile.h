@@ -471,7 +471,8 @@ int sg_context_workspace_bytes(const sg_context_problem* p, int32_t n_tiles, siz
  * Cross attention of tiles to an encoder's states.  For tile i, head a and query n:
  *     O[a][n][:] = sum_m softmax_m( scale * <Q[a][n], K[a'][m]> ) * V[a'][m][:],   a' = a / (heads / kv_heads)
  * over the places m < ctx_len[i] of tile i's context with key_mask[i][m] != 0.  A query without any such place, or whose
- * scores are all -inf, gives zeros.  Keys and values at other places are not read: they may hold anything.
+ * scores are all -inf, gives zeros.  Keys and values at other places do not count, whatever they hold
+ * (NaN, infinities); those behind the length are not read.
  *   q, out     host arrays of n_tiles device pointers: queries and outputs of a tile
  *   k, v       host arrays of n_tiles device pointers: the context of each tile; tiles with the same prompt name the same
  *              buffers.  With ctx_tokens = 0 they are not looked at (NULL is fine)

@@ -61,7 +61,9 @@ __global__ __launch_bounds__(256 * WAYS, 2) void context_bf16_wide_kernel(const 
     const Segment& g = second ? g1 : g0;
     const int key0 = (second ? from + j - n0 : from + j) * kKeys;
     const uint32_t dst = lds0 + (is_v ? 2 * kHalf : 0) + (j & 1) * kHalf + first * kSlot;
-    move_half<D, kInstr>(is_v ? g.v : g.k, g.token, key0, first, v, is_v, dst);
+    // (masked keys inside the segment may come along, their scores are replaced; masked values may not: 0 times a NaN is a NaN)
+    const uint64_t take = !is_v && key0 + kKeys <= g.len ? ~0ull : v;
+    move_half<D, kInstr>(is_v ? g.v : g.k, g.token, key0, first, take, is_v, dst);
   };
   // which of its keys count
   auto counting = [&](int j) SG_INLINE -> uint64_t {
