@@ -527,8 +527,9 @@ typedef struct sg_norm_problem {
  *              row or over each 128 channels of it (0 where that maximum is below 2^-100: zeros are written).  Aliases nothing
  *   out_scale  SG_F8_E4M3: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats; else NULL
  *   run        device, n_tiles bytes, or NULL: all tiles
- * y is computed from the sum before it is rounded, in fp32; |s| below 2^60 (the squares are summed in fp32).  A row with a NaN is
- * NaN throughout.  All pointers 16-byte aligned (out_scale: 4).
+ * y is computed from the sum before it is rounded, in fp32, for every finite s: where the sum of the squares would leave the fp32 range, it is taken
+ * of the scaled row.  With eps = 0 a row of zeros gives NaN (0 / 0).  A row with a NaN is NaN throughout, one with an infinity
+ * NaN there and 0 elsewhere.  All pointers 16-byte aligned (out_scale: 4).
  */
 int sg_tile_residual_norm(const sg_norm_problem* p, int32_t n_tiles, const void* const* x, const void* const* residual,
                           const void* weight, const uint8_t* run, void* const* sum, void* const* out,

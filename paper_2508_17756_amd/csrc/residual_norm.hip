@@ -60,13 +60,17 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
 constexpr float kE4m3Max = 448.f;
 // Blocks whose largest value is below this are written as zeros with a scale of 0: 448 / a has to stay finite.
 constexpr float kLeast = 7.888609052210118e-31f;   // 2^-100
+// Mean squares outside kLeast .. the largest fp32 number are taken again of the row scaled by a power of two, so that neither a square nor their sum
+// leaves the range: |s| 2^-72 is below 2^56, 32,768 squares of it below 2^127; and with a mean below 2^-100 and up to 32,768 channels |s| 2^100 is below
+// 2^58, the square of the smallest fp32 number 2^-98.  (From kLeast on what squares below 2^-149 lack is below 2^-49 of the mean.)
+constexpr float kShrink = 2.117582368135751e-22f, kGrow = 1.2676506002282294e30f;   // 2^-72, 2^100
 
 // T: stored type; E4M3: output in 8 bits; VPL: vectors per lane; WAVES: wavefronts per row (1: four wavefronts of a workgroup take rows
 // of their own)
 template <typename T, bool E4M3, int VPL, int WAVES>
 __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel(const NormArgs a, const NormTable tab) {
   constexpr int kThreads = WAVES == 16 ? 1024 : 256;
-  __shared__ float shared[2][2][WAVES];   // [parity of the row][sum, maximum]
+  __shared__ float shared[2][3][WAVES];   // [parity of the row][sum, maximum, sum of the scaled row]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int lanes = WAVES > 1 ? 64 * WAVES : a.lanes;             // per row
   const int first = WAVES > 1 ? (int)threadIdx.x : lane & (lanes - 1);
@@ -87,8 +91,10 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel
     }
     return v;
   };
-  auto row_sum = [&](float v) { return across(v, 0, [](float x, float y) { return x + y; }); };
+  auto row_sum = [&](float v, int what) { return across(v, what, [](float x, float y) { return x + y; }); };
   auto row_max = [&](float v) { return across(v, 1, [](float x, float y) { return fmaxf(x, y); }); };
+  // What a row has one of: of a row of whole wavefronts in a scalar register (fp32 rows of 20,480 channels to e4m3 254 -> 246 us).
+  auto of_row = [](float v) { return WAVES > 1 ? __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))) : v; };
   Vec8<T> w[VPL];
 #pragma unroll
   for (int i = 0; i < VPL; ++i)
@@ -121,12 +127,34 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel
         sq += s[i][e] * s[i][e];
       }
     }
-    const float norm = rsqrtf(row_sum(sq) / (float)a.channels + a.eps);
+    const float mean = of_row(row_sum(sq, 0) / (float)a.channels + a.eps);
+    float norm = of_row(rsqrtf(mean)), by = 1.f;   // y = s * by * norm * w
+    const bool odd = !(mean >= kLeast && mean <= 3.402823466e38f);   // (a NaN too; the lanes of a row agree, rows that share a wavefront may not)
+    const bool any_odd = WAVES > 1 ? odd : __any(odd);
+    if (any_odd) {
+      const float to = mean < kLeast ? kGrow : kShrink;
+      float again = 0.f;
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) again += (s[i][e] * to) * (s[i][e] * to);
+      again = rsqrtf(row_sum(again, 2) / (float)a.channels + a.eps * to * to);
+      if (odd) {
+        by = to;
+        norm = of_row(again);
+      }
+    }
     if (a.has_sum) {
       T* const o = (T*)tab.sum[tile] + row * a.s_stride;
 #pragma unroll
       for (int i = 0; i < VPL; ++i)
         if (there && first + i * lanes < a.n_vec) store8(o + 8 * (first + i * lanes), s[i]);
+    }
+    if (any_odd) {
+#pragma unroll
+      for (int i = 0; i < VPL; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[i][e] *= by;
     }
 #pragma unroll
     for (int i = 0; i < VPL; ++i)
