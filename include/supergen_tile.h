@@ -524,7 +524,8 @@ typedef struct sg_norm_problem {
  *   weight     device, `channels` elements, or NULL: ones
  *   sum        host array: s in the tensors' type, or NULL.  sum[i] may be x[i] or residual[i] (with its stride): in place
  *   out        host array: y in the tensors' type; or, with SG_F8_E4M3, y / scale rounded to 8 bits, scale = max|y| / 448 over a
- *              row or over each 128 channels of it (0 where that maximum is below 2^-100: zeros are written).  Aliases nothing
+ *              row or over each 128 channels of it (0 where that maximum is below 2^-100: zeros are written; NaN, as all 8-bit values of the row
+ *              or block, where one of them is).  Aliases nothing
  *   out_scale  SG_F8_E4M3: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats; else NULL
  *   run        device, n_tiles bytes, or NULL: all tiles
  * y is computed from the sum before it is rounded, in fp32, for every finite s: where the sum of the squares would leave the fp32 range, it is taken

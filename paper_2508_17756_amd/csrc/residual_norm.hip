@@ -57,6 +57,9 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
   *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 
+// The larger of two numbers; NaN where one is (fmaxf gives the other one, and a block with a NaN would have a scale that hides it).
+__device__ __forceinline__ float nan_max(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 constexpr float kE4m3Max = 448.f;
 // Blocks whose largest value is below this are written as zeros with a scale of 0: 448 / a has to stay finite.
 constexpr float kLeast = 7.888609052210118e-31f;   // 2^-100
@@ -92,7 +95,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel
     return v;
   };
   auto row_sum = [&](float v, int what) { return across(v, what, [](float x, float y) { return x + y; }); };
-  auto row_max = [&](float v) { return across(v, 1, [](float x, float y) { return fmaxf(x, y); }); };
+  auto row_max = [&](float v) { return across(v, 1, [](float x, float y) { return nan_max(x, y); }); };
   // What a row has one of: of a row of whole wavefronts in a scalar register (fp32 rows of 20,480 channels to e4m3 254 -> 246 us).
   auto of_row = [](float v) { return WAVES > 1 ? __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))) : v; };
   Vec8<T> w[VPL];
@@ -175,12 +178,12 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel
       for (int i = 0; i < VPL; ++i) {
         most[i] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) most[i] = fmaxf(most[i], fabsf(s[i][e]));
+        for (int e = 0; e < 8; ++e) most[i] = nan_max(most[i], fabsf(s[i][e]));
       }
       if (a.group_vecs == 0) {
         float m = most[0];
 #pragma unroll
-        for (int i = 1; i < VPL; ++i) m = fmaxf(m, most[i]);
+        for (int i = 1; i < VPL; ++i) m = nan_max(m, most[i]);
         m = row_max(m);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) most[i] = m;
@@ -190,7 +193,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void residual_norm_kernel
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
 #pragma unroll
-          for (int d = 1; d < 16; d <<= 1) most[i] = fmaxf(most[i], __shfl_xor(most[i], d, 64));
+          for (int d = 1; d < 16; d <<= 1) most[i] = nan_max(most[i], __shfl_xor(most[i], d, 64));
           const int v = first + i * lanes;
           if (there && v < a.n_vec && (v & 15) == 0) scales[row * groups + (v >> 4)] = most[i] < kLeast ? 0.f : most[i] / kE4m3Max;
         }

@@ -1,4 +1,4 @@
-"""The residual norm over the whole range of its types: squares whose sum leaves the fp32 range on either side."""
+"""The residual norm over the whole range of its types: squares whose sum leaves the fp32 range on either side, scales of rows with a NaN."""
 import pytest
 import torch
 
@@ -85,3 +85,59 @@ def test_a_row_of_zeros_without_eps_is_nan_and_with_any_eps_zeros():
             torch.cuda.synchronize()
             assert bool(torch.isnan(y[[0, 2]]).all()) if eps == 0 else bool((y[[0, 2]] == 0).all())
             assert float((y[1] - 1).abs().max()) < 1e-5
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("channels", CHANNELS[1:])
+@pytest.mark.parametrize("group", [0, 128])
+def test_scales_of_rows_with_a_nan(dtype, channels, group):
+    """Codes and scales both: what leaves out blocks whose scale is 0 must not lose a NaN.  A NaN in the weight is one of its block."""
+    x = _rows(channels, dtype, [1.0] * 9, 4)
+    x[2, channels // 2] = float("nan")
+    x[5, channels - 1] = float("nan")
+    x[7] = 0
+    w = torch.ones(channels, device="cuda").to(x.dtype)
+    p = sg.make_norm_problem(9, channels, dtype, out_dtype="e4m3", scale_group=group)
+    y = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device="cuda")
+    scale = torch.empty((9, channels // group if group else 1), device="cuda")
+
+    def call():
+        sg.sg_tile_residual_norm(p, [x], w, [y], out_scale=[scale])
+        torch.cuda.synchronize()
+        return y.float().cpu(), scale.cpu()
+
+    code, sc = call()
+    for row in range(9):
+        if row in (2, 5):
+            assert bool(torch.isnan(code[row]).all()) and bool(torch.isnan(sc[row]).all())
+        else:
+            assert bool(torch.isfinite(code[row]).all()) and bool(torch.isfinite(sc[row]).all())
+    assert float(sc[7].max()) == 0 and float(code[7].abs().max()) == 0
+    w[3] = float("nan")
+    code, sc = call()
+    width = group or channels
+    assert bool(torch.isnan(code[0, 3])) and bool(torch.isnan(sc[:, 0]).all())
+    assert bool(torch.isfinite(sc[0, 1:]).all()) and bool(torch.isfinite(code[0, width:]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("channels", CHANNELS[1:])
+def test_a_row_with_an_infinity(dtype, channels):
+    """Infinity over infinity is NaN, numbers over infinity are 0; in 8 bits the block of the infinity is NaN."""
+    x = _rows(channels, dtype, [1.0] * 5, 5)
+    x[1, channels - 2] = -float("inf")
+    for group in (None, 0, 128):
+        p = sg.make_norm_problem(5, channels, dtype, out_dtype=None if group is None else "e4m3", scale_group=group or 0)
+        y = torch.empty(x.shape, dtype=x.dtype if group is None else torch.float8_e4m3fn, device="cuda")
+        scale = None if group is None else [torch.empty((5, channels // group if group else 1), device="cuda")]
+        sg.sg_tile_residual_norm(p, [x], None, [y], out_scale=scale)
+        torch.cuda.synchronize()
+        got = y.float().cpu()
+        want = torch.zeros(x.shape, dtype=torch.bool)
+        if group is None:
+            want[1, channels - 2] = True
+        else:
+            want[1, channels - (group or channels):] = True
+            assert bool(torch.isnan(scale[0][1, -1])) and bool(torch.isfinite(scale[0][[0, 2, 3, 4]]).all())
+        assert torch.equal(torch.isnan(got), want)
+        assert bool((got[1][~want[1]] == 0).all())
