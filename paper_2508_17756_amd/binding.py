@@ -529,21 +529,42 @@ def _pointers(tensors, n):
     return _ptr_array(tensors)
 
 
+def _vector(t, kinds, n, name):
+    """Address of the device array whose first n elements the library reads.  Another type (lengths in int64, torch's default for integers),
+    strides, too few elements or host memory would be read as something else without a word."""
+    if t.dtype not in kinds:
+        raise TypeError("%s must be %s, not %s" % (name, " or ".join(str(k) for k in kinds), t.dtype))
+    if not t.is_contiguous() or t.numel() < n:
+        raise ValueError("%s must be contiguous and hold %d elements" % (name, n))
+    if not t.is_cuda:
+        raise ValueError("%s must be in device memory" % name)
+    return t.data_ptr()
+
+
+def _lengths(t, n, name):
+    return None if t is None else _vector(t, (_torch().int32,), n, name)
+
+
+def _flags(t, n, name):
+    return None if t is None else _vector(t, (_torch().uint8, _torch().bool), n, name)
+
+
 def sg_tile_cross_attention(p, q, k, v, out, ctx_len=None, key_mask=None, run=None, workspace=None):
-    """q, k, v, out: lists of one tensor per tile (k, v: None if the context has no tokens); ctx_len: int32, key_mask and run: uint8."""
+    """q, k, v, out: lists of one tensor per tile (k, v: None if the context has no tokens); ctx_len: int32, key_mask and run: uint8 or bool."""
     n = len(q)
-    st = load_library().sg_tile_cross_attention(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _pointers(v, n), _ptr(ctx_len),
-                                                _ptr(key_mask), _ptr(run), _pointers(out, n), *_scratch(workspace), _stream())
+    st = load_library().sg_tile_cross_attention(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _pointers(v, n),
+                                                _lengths(ctx_len, n, "ctx_len"), _flags(key_mask, n * p.ctx_tokens, "key_mask"),
+                                                _flags(run, n, "run"), _pointers(out, n), *_scratch(workspace), _stream())
     _check(st, "sg_tile_cross_attention")
     return out
 
 
 def sg_tile_prefix_attention(p, q, k, v, prefix_k, prefix_v, out, own_len=None, prefix_len=None, run=None, workspace=None):
-    """q, k, v, out: lists of one tensor per tile (k, v: None if tiles have no keys of their own); own_len, prefix_len: int32; run: uint8."""
+    """q, k, v, out: lists of one tensor per tile (k, v: None if tiles have no keys of their own); own_len, prefix_len: int32; run: uint8 or bool."""
     n = len(q)
     st = load_library().sg_tile_prefix_attention(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _pointers(v, n), _ptr(prefix_k),
-                                                 _ptr(prefix_v), _ptr(own_len), _ptr(prefix_len), _ptr(run), _pointers(out, n),
-                                                 *_scratch(workspace), _stream())
+                                                 _ptr(prefix_v), _lengths(own_len, n, "own_len"), _lengths(prefix_len, 1, "prefix_len"),
+                                                 _flags(run, n, "run"), _pointers(out, n), *_scratch(workspace), _stream())
     _check(st, "sg_tile_prefix_attention")
     return out
 
@@ -556,9 +577,10 @@ def make_norm_problem(rows, channels, dtype, out_dtype=None, scale_group=0, eps=
 
 
 def sg_tile_residual_norm(p, x, weight, out, residual=None, sum_out=None, out_scale=None, run=None):
-    """x, out, residual, sum_out, out_scale: lists of one tensor per tile, the last three or None; weight: `channels` elements or None."""
+    """x, out, residual, sum_out, out_scale: lists of one tensor per tile, the last three or None; weight: `channels` elements or None; run: uint8
+    or bool."""
     n = len(x)
-    st = load_library().sg_tile_residual_norm(ctypes.byref(p), n, _ptr_array(x), _pointers(residual, n), _ptr(weight), _ptr(run),
-                                              _pointers(sum_out, n), _pointers(out, n), _pointers(out_scale, n), _stream())
+    st = load_library().sg_tile_residual_norm(ctypes.byref(p), n, _ptr_array(x), _pointers(residual, n), _ptr(weight),
+                                              _flags(run, n, "run"), _pointers(sum_out, n), _pointers(out, n), _pointers(out_scale, n), _stream())
     _check(st, "sg_tile_residual_norm")
     return out
