@@ -522,7 +522,8 @@ typedef struct sg_norm_problem {
  * Residual addition and root-mean-square norm:  s = x + residual,  y = s * rsqrt(mean(s^2) + eps) * weight  per row.
  *   residual   host array of n_tiles device pointers, or NULL: s = x
  *   weight     device, `channels` elements, or NULL: ones
- *   sum        host array: s in the tensors' type, or NULL.  sum[i] may be x[i] or residual[i] (with its stride): in place
+ *   sum        host array: s in the tensors' type, or NULL.  sum[i] may be x[i] or residual[i] (with its stride): in place.  No other tile may have
+ *              that buffer as x, residual or sum (tiles that do not write in place may share x and residual)
  *   out        host array: y in the tensors' type; or, with SG_F8_E4M3, y / scale rounded to 8 bits, scale = max|y| / 448 over a
  *              row or over each 128 channels of it (0 where that maximum is below 2^-100: zeros are written; NaN, as all 8-bit values of the row
  *              or block, where one of them is).  Aliases nothing

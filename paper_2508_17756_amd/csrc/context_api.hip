@@ -1,5 +1,7 @@
 // C ABI of the operators beside a tile's self-attention: host-side argument checks and the order of launches.
+#include <algorithm>
 #include <cmath>
+#include <utility>
 #include "context_common.h"
 
 namespace sg {
@@ -41,6 +43,22 @@ static int check_tiles(const void* const* a, int n) {
   for (int i = 0; i < n; ++i)
     if (!a[i] || !aligned16(a[i])) return SG_ERR_INVALID_ARG;
   return SG_OK;
+}
+
+// In-place sums: sum[i] may be x[i] or residual[i], with its stride, and nothing of another tile, whose rows other workgroups read and write meanwhile.
+static bool sums_apart(const sg_norm_problem& p, int n, const void* const* x, const void* const* residual, void* const* sum) {
+  std::pair<const void*, int> at[SG_MAX_TILES];
+  for (int i = 0; i < n; ++i) at[i] = {sum[i], i};
+  std::sort(at, at + n);
+  for (int i = 1; i < n; ++i)
+    if (at[i].first == at[i - 1].first) return false;
+  auto reads = [&](const void* from, int i, int64_t stride) {
+    const auto found = std::lower_bound(at, at + n, std::make_pair(from, 0));
+    return found == at + n || found->first != from || (found->second == i && stride == p.sum_stride);
+  };
+  for (int i = 0; i < n; ++i)
+    if (!reads(x[i], i, p.x_stride) || (residual && !reads(residual[i], i, p.residual_stride))) return false;
+  return true;
 }
 
 static size_t workspace_bytes(const sg_context_problem& p, bool prefix, int n_tiles) {
@@ -167,7 +185,7 @@ int sg_tile_residual_norm(const sg_norm_problem* p, int32_t n_tiles, const void*
   if (n_tiles == 0 || p->rows == 0) return SG_OK;
   if (check_tiles(x, n_tiles) != SG_OK || check_tiles((const void* const*)out, n_tiles) != SG_OK) return SG_ERR_INVALID_ARG;
   if (residual && check_tiles(residual, n_tiles) != SG_OK) return SG_ERR_INVALID_ARG;
-  if (sum && check_tiles((const void* const*)sum, n_tiles) != SG_OK) return SG_ERR_INVALID_ARG;
+  if (sum && (check_tiles((const void* const*)sum, n_tiles) != SG_OK || !sums_apart(*p, n_tiles, x, residual, sum))) return SG_ERR_INVALID_ARG;
   if (weight && !aligned16(weight)) return SG_ERR_INVALID_ARG;
   if ((p->out_dtype == SG_F8_E4M3) != (out_scale != nullptr)) return SG_ERR_INVALID_ARG;
   if (out_scale)
