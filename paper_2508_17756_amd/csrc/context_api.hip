@@ -24,11 +24,12 @@ static int validate(const sg_context_problem* p) {
       (p->ctx_tokens > 0 && !stride_ok(p->ctx_stride_token, p->ctx_stride_head, d)) ||
       (p->own_tokens > 0 && !stride_ok(p->own_stride_token, p->own_stride_head, d)))
     return SG_ERR_INVALID_ARG;
-  if (p->out_stride_head < d && p->heads > 1) return SG_ERR_INVALID_ARG;
-  // outputs that overlap: heads lie behind all tokens of the one before, or inside a token
-  if (p->heads > 1 && p->tokens > 1 && p->out_stride_head < (int64_t)(p->tokens - 1) * p->out_stride_token + d &&
-      p->out_stride_token < (int64_t)(p->heads - 1) * p->out_stride_head + d)
-    return SG_ERR_INVALID_ARG;
+  // outputs that overlap: heads lie behind all tokens of the one before, or inside a token (in quotients: the products can pass 64 bits)
+  if (p->heads > 1) {
+    if (p->out_stride_head < d) return SG_ERR_INVALID_ARG;
+    if ((p->out_stride_head - d) / p->out_stride_token < p->tokens - 1 && (p->out_stride_token - d) / p->out_stride_head < p->heads - 1)
+      return SG_ERR_INVALID_ARG;
+  }
   if (d != 64 && d != 128) return SG_ERR_UNSUPPORTED;
   // offsets inside a stage of 64 keys are 32-bit; rows and items are numbered in 32 bits, for 64 tiles a launch
   if ((p->ctx_tokens > 0 && p->ctx_stride_token >= (1ll << 22)) || (p->own_tokens > 0 && p->own_stride_token >= (1ll << 22)))
