@@ -443,7 +443,8 @@ int sg_refine_step_canvas(const sg_problem* p, const void* q, const void* k, con
  * so that [heads][tokens][d] and [tokens][heads][d] (what a projection leaves) are both expressible.  Keys and values of one
  * segment share their strides (those of a segment of 0 tokens are not looked at).  All strides are positive multiples of 8,
  * stride_token >= head_dim and below 2^22 for keys; heads * tokens is below 2^25, kv_heads at most 65,535, each segment below
- * 2^30 tokens; base pointers are 16-byte aligned. */
+ * 2^30 tokens; 64 tiles have less than 2^24 - 8 blocks of 128 (fp32: 64) queries per head of keys, ends counted as whole ones; base pointers
+ * are 16-byte aligned. */
 typedef struct sg_context_problem {
   int32_t heads, kv_heads;    /* heads of the queries; of keys and values: a divisor of heads (head a reads a / (heads / kv_heads)) */
   int32_t head_dim;           /* 64 or 128                                                                       */

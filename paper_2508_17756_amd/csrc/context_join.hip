@@ -60,7 +60,7 @@ void cut_wide(CtxPart& p, int batches, int64_t rows, int kv_heads, int64_t stage
   p.splits = (int32_t)splits;
   p.rows = (int32_t)rows;
   p.row_blocks = (int32_t)blocks;
-  p.items = base * splits > (1 << 30) ? -1 : (int32_t)(base * splits);
+  p.items = base * splits > (1 << 24) - 8 ? -1 : (int32_t)(base * splits);   // a grid has less than 2^32 threads, 256 a workgroup
 }
 
 }  // namespace
