@@ -481,9 +481,10 @@ int sg_context_workspace_bytes(const sg_context_problem* p, int32_t n_tiles, siz
  *   key_mask   device, [n_tiles][ctx_tokens] bytes, 0 = the place does not count, or NULL
  *   run        device, n_tiles bytes (sg_cache_gate's recompute), or NULL: all tiles
  * bf16 problems multiply in bf16 on the matrix cores (probabilities are rounded to bf16 for the second product), accumulate
- * in fp32 and scale the scores in fp32 behind the product; f32 problems multiply and accumulate in fp32.  A NaN in Q, or at a
- * place that counts in K or V, reaches every output that depends on it, and no other.  The exponentials' reference follows the
- * largest score to within 2^5, so that sums of p v stay finite where 32 * keys * |v| does.  Tiles are attended up to 64 a launch; calls
+ * in fp32 and scale the scores in fp32 behind the product: scaled scores are below 2^127 in size, probabilities below 2^-126 of the
+ * reference count as 0.  f32 problems multiply and accumulate in fp32, Q multiplied by the scale first, and take any finite scores; every
+ * probability that fp32 holds counts.  A NaN in Q, or at a place that counts in K or V, reaches every output that depends on it, and no other.  The
+ * exponentials' reference follows the largest score (bf16: to within 2^5), so that sums of p v stay finite where 32 * keys * |v| does.  Tiles are attended up to 64 a launch; calls
  * whose queries do not fill the device are cut along the keys and joined by a second launch.  The same call gives the same bits
  * every time; a call of other sizes, or of more tiles, may be cut in another way and round differently.
  */

@@ -104,8 +104,19 @@ __device__ __forceinline__ CtxRowEnd ctx_row_end(const CtxArgs& a, const CtxTabl
   return {r.there ? (uint64_t)(uintptr_t)o : 0, r.rid};
 }
 
-// A row's shares in the workspace, (reference in the log2 domain, sum of probabilities) and sums of p v, joined to what (top, sum, acc) holds: four
+// What a share whose reference is `ref` counts against one of `top` >= ref.  bf16 keeps references in the log2 domain.  fp32 keeps the scores'
+// own, of which only differences are multiplied by log2(e), so that scores up to the largest number stay finite, and takes the function that returns
+// results below 2^-126: times a value near the largest number they still count.
+constexpr float kLog2e = 1.4426950408889634f;
+template <typename OUT>
+__device__ __forceinline__ float ctx_weight(float ref, float top) {
+  if constexpr (sizeof(OUT) == 4) return exp2f((ref - top) * kLog2e);
+  else return __builtin_amdgcn_exp2f(ref - top);
+}
+
+// A row's shares in the workspace, (reference, sum of probabilities) and sums of p v, joined to what (top, sum, acc) holds: four
 // channels a lane.  The loads of 16 shares are in flight together; one share after the other, 32 of them took 25 us.
+template <typename OUT>
 __device__ __forceinline__ void ctx_add_shares(const f32x2* ml, const float* sums, int64_t stride, int n, float& top, float& sum, f32x4& acc) {
   constexpr int kBatch = 16;
   for (int k = 0; k < n; k += kBatch) {
@@ -120,14 +131,14 @@ __device__ __forceinline__ void ctx_add_shares(const f32x2* ml, const float* sum
     float most = top;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) most = fmaxf(most, x[u][0]);
-    const float keep = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - most);
+    const float keep = sum == 0.f ? 0.f : ctx_weight<OUT>(top, most);
     top = most;
     sum *= keep;
     acc *= keep;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
       // a share without keys counts for nothing (one whose scores are all NaN has a reference of -inf as well, but a sum)
-      const float e = k + u >= n || x[u][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(x[u][0] - top);
+      const float e = k + u >= n || x[u][1] == 0.f ? 0.f : ctx_weight<OUT>(x[u][0], top);
       sum += e * x[u][1];
       acc += e * v[u];
     }
@@ -135,7 +146,7 @@ __device__ __forceinline__ void ctx_add_shares(const f32x2* ml, const float* sum
 }
 
 // The end of a call whose wavefronts attended shares of the keys.  A wavefront's LDS holds its sums, ROWS x D floats (16-byte chunk c of row r at chunk
-// c ^ (r & 15)), at `sums` (reference in the log2 domain, sum) of the rows and at `ends` their CtxRowEnd.  The WAYS wavefronts of a row block join
+// c ^ (r & 15)), at `sums` (reference, sum) of the rows and at `ends` their CtxRowEnd.  The WAYS wavefronts of a row block join
 // their shares, and those of an earlier launch, and write the results or, for a later join, their share.  Four rows at a time, so that their reads
 // overlap: one after the other, 32 rows took 5 us.
 template <typename OUT, int D, int ROWS, int WAYS>
@@ -172,12 +183,12 @@ __device__ __forceinline__ void ctx_finish(const CtxArgs& a, const CtxPart& p, u
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < WAYS; ++w) {
-        const float e = ml[i][w][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[i][w][0] - top);   // 0: no keys (NaN scores leave a sum)
+        const float e = ml[i][w][1] == 0.f ? 0.f : ctx_weight<OUT>(ml[i][w][0], top);   // 0: no keys (NaN scores leave a sum)
         sum += e * ml[i][w][1];
         acc += e * o[i][w];
       }
       const int64_t shares = (int64_t)(int)end[i][2] * a.n_shares;
-      if (p.prior) ctx_add_shares((const f32x2*)(a.shares + all * D) + shares, a.shares + shares * D + 4 * chunk, D, p.prior, top, sum, acc);
+      if (p.prior) ctx_add_shares<OUT>((const f32x2*)(a.shares + all * D) + shares, a.shares + shares * D + 4 * chunk, D, p.prior, top, sum, acc);
       if (a.n_shares == p.prior) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         if constexpr (sizeof(OUT) == 4) *(f32x4*)((OUT*)(uintptr_t)to + 4 * chunk) = acc * inv;

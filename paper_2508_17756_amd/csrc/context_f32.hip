@@ -8,10 +8,10 @@
 // bytes at a time.
 //
 // Two forms.  Shared: the 4 wavefronts of a workgroup take 16 rows each against the same stages of keys, for calls with rows to fill the
-// chip (32 each read fewer fragments, which do not bind, and end less evenly: 116 us for the 110 below).  Otherwise every wavefront streams keys of its own through LDS of its own; wavefronts of a workgroup take other row blocks or other
+// chip (32 each read fewer fragments, which do not bind, and end less evenly: 116 us for 110).  Otherwise every wavefront streams keys of its own through LDS of its own; wavefronts of a workgroup take other row blocks or other
 // shares of the keys, whichever there are more of (context_common.h).
 //
-// Bound by the fp32 matrix instruction where there are rows (4 tiles of 2,880, 8 heads x 128, 226 keys: 110 us, 97 TFLOP/s; a large product of
+// Bound by the fp32 matrix instruction where there are rows (4 tiles of 2,880, 8 heads x 128, 226 keys: 112 us, 95 TFLOP/s; a large product of
 // the library 154), by latency where there are few (4 tiles of 300, 2 heads x 64, 377 keys: 10.4 us).
 #include <atomic>
 #include "context_common.h"
@@ -24,7 +24,6 @@ namespace {
 // A wavefront's LDS: two stages of 8 KiB of keys and 8 KiB of values; after the keys its sums (rows x D floats), then (reference, sum) of the rows and where they go.
 constexpr int kHalfStage = 8192, kStage = 2 * kHalfStage, kWaveLds = 2 * kStage, kLds = 4 * kWaveLds;
 constexpr int kSumsAt = kStage, kRowsAt = kSumsAt + 512;
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct Segment {
   const char* k;
@@ -226,20 +225,41 @@ __global__ __launch_bounds__(256, SHARED ? 3 : 1) void context_f32_kernel(const 
         mx = group_max(mx);
         const float top = fmaxf(m[qb], mx);
         if (__any(top != m[qb])) {
-          const float alpha = m[qb] == top ? 1.f : __builtin_amdgcn_exp2f((m[qb] - top) * kLog2e);   // first keys: exp2(-inf) = 0
+          const float alpha = m[qb] == top ? 1.f : exp2f((m[qb] - top) * kLog2e);   // first keys: exp2(-inf) = 0
           m[qb] = top;
           l[qb] *= alpha;
 #pragma unroll
           for (int db = 0; db < D / 16; ++db) o[qb][db] *= alpha;
         }
         const float ref = m[qb] == -__builtin_inff() ? 0.f : m[qb];   // no key so far: probabilities 0
+        // The exponential instruction returns 0 for results below 2^-126.  Where a score lies that far below the reference (or at -inf), the
+        // function that returns them is called: times a value near the largest number they still count.  (4 tiles of 2,880, 8 heads x 128, 226 keys
+        // 110.3 -> 112.4 us, 4 of 300, 2 heads x 64, 377 keys 10.2 -> 10.4.)
+        float mn = s[qb][0][0];
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            s[qb][b][r] = __builtin_amdgcn_exp2f((s[qb][b][r] - ref) * kLog2e);
-            l[qb] += s[qb][b][r];
-          }
+          for (int r = 0; r < 4; ++r) mn = fminf(mn, s[qb][b][r]);
+        const bool far = __any(mn - ref < -87.f);
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[qb][b][r] = (s[qb][b][r] - ref) * kLog2e;
+        if (__builtin_expect(far, 0)) {
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[qb][b][r] = exp2f(s[qb][b][r]);
+        } else {
+#pragma unroll
+          for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[qb][b][r] = __builtin_amdgcn_exp2f(s[qb][b][r]);
+        }
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) l[qb] += s[qb][b][r];
       }
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b)
@@ -271,7 +291,7 @@ __global__ __launch_bounds__(256, SHARED ? 3 : 1) void context_f32_kernel(const 
         const int64_t at = (int64_t)end[qb].rid * a.n_shares + p.first_share + split;
         const int64_t all = (int64_t)a.n_tiles * a.heads * a.tokens * a.n_shares;
         dst = a.shares + at * D + 16 * grp;
-        if (grp == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{m[qb] * kLog2e, l[qb]};
+        if (grp == 0) *(f32x2*)(a.shares + all * D + at * 2) = f32x2{m[qb], l[qb]};
       }
 #pragma unroll
       for (int h = 0; h < D / 64; ++h)
@@ -289,7 +309,7 @@ __global__ __launch_bounds__(256, SHARED ? 3 : 1) void context_f32_kernel(const 
         for (int r = 0; r < 4; ++r)
           *(SG_LDS f32x4*)(uintptr_t)(mine + (16 * qb + lq) * (D * 4) + (((16 * h + 4 * grp + r) ^ lq) << 4)) = four(qb, h, r);
       if (grp == 0) {
-        *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + (16 * qb + lq) * 8) = f32x2{m[qb] * kLog2e, l[qb]};
+        *(SG_LDS f32x2*)(uintptr_t)(mine + kSumsAt + (16 * qb + lq) * 8) = f32x2{m[qb], l[qb]};
         *(SG_LDS u32x4*)(uintptr_t)(mine + kRowsAt + (16 * qb + lq) * 16) = u32x4{(uint32_t)end[qb].out, (uint32_t)(end[qb].out >> 32), (uint32_t)end[qb].rid, 0u};
       }
     }

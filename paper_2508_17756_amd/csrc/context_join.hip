@@ -1,6 +1,6 @@
 // How a call of sg_tile_cross_attention / sg_tile_prefix_attention is cut into work, and the join of the shares of a row that
 // different workgroups attended:
-//     M = max m_s,   o = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s     over the shares s of (reference m, sum l, sums O of p v)
+//     M = max m_s,   o = sum_s e^(m_s - M) O_s / sum_s e^(m_s - M) l_s     over the shares s of (reference m, sum l, sums O of p v)
 // in the order of the shares, so that a call gives the same bits every time.
 #include "context_common.h"
 
@@ -20,7 +20,7 @@ __global__ __launch_bounds__(256) void context_join_kernel(const CtxArgs a, cons
   const f32x2* const ml = (const f32x2*)(a.shares + n_rows * a.n_shares * D) + rid * a.n_shares;
   float top = -__builtin_inff(), sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  ctx_add_shares(ml, sums, D, a.n_shares, top, sum, acc);
+  ctx_add_shares<OUT>(ml, sums, D, a.n_shares, top, sum, acc);
   const f32x4 y = sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc / sum;
   OUT* const out = (OUT*)tab.out[tile] + (int64_t)head * a.o_head + (int64_t)token * a.o_token + 4 * chunk;
   if constexpr (sizeof(OUT) == 4) *(f32x4*)out = y;
