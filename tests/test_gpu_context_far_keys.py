@@ -1,4 +1,5 @@
-"""fp32 context attention, keys far below the largest score: probabilities below 2^-126 count, in every kernel and in every join."""
+"""Context attention, keys far below the largest score: fp32 probabilities below 2^-126 count, in every kernel and in every join; scores at -inf have
+probability 0."""
 import pytest
 import torch
 
@@ -7,12 +8,12 @@ from context_util import Call
 pytestmark = pytest.mark.gpu
 
 
-def _cross(tiles, tokens, heads, d, ctx):
-    return lambda: Call(tiles, tokens, heads, heads, d, "f32", ctx)
+def _cross(tiles, tokens, heads, d, ctx, dtype="f32"):
+    return lambda: Call(tiles, tokens, heads, heads, d, dtype, ctx)
 
 
-def _prefix(tiles, tokens, heads, kv_heads, d, prefix, own):
-    return lambda: Call(tiles, tokens, heads, kv_heads, d, "f32", prefix, own=own, prefix=True)
+def _prefix(tiles, tokens, heads, kv_heads, d, prefix, own, dtype="f32"):
+    return lambda: Call(tiles, tokens, heads, kv_heads, d, dtype, prefix, own=own, prefix=True)
 
 
 # as many rows as 16 or 32 to a wavefront, as workgroups that share their keys take; keys cut inside a workgroup, over workgroups, over launches
@@ -72,3 +73,38 @@ def test_scores_near_the_largest_number(name, make):
     torch.cuda.synchronize()
     for o in out:
         assert float((o - 1).abs().max()) <= (n + 64) * 2.0 ** -24
+
+
+BF16_CALLS = [("bf16_token", _cross(1, 1, 8, 64, 77, "bf16")), ("bf16_split", _cross(2, 100, 8, 128, 300, "bf16")),
+              ("bf16_split_joined", _cross(1, 1024, 2, 128, 2000, "bf16")), ("bf16_wide_128", _cross(4, 600, 10, 128, 600, "bf16")),
+              ("bf16_wide_64", _cross(4, 700, 24, 64, 700, "bf16")), ("bf16_wide_cut", _cross(1, 1024, 2, 128, 8000, "bf16")),
+              ("bf16_two_groups", _cross(1, 1024, 32, 64, 512, "bf16")), ("bf16_resident_64", _cross(1, 2048, 64, 64, 512, "bf16")),
+              ("bf16_resident_128", _cross(1, 2048, 64, 128, 256, "bf16")), ("bf16_stacked", _prefix(20, 1, 40, 8, 128, 2000, 40, "bf16")),
+              ("bf16_stacked_cut", _prefix(20, 4, 4, 1, 128, 2000, 700, "bf16"))]
+
+
+@pytest.mark.parametrize("name, make", CALLS + BF16_CALLS, ids=[c[0] for c in CALLS + BF16_CALLS])
+def test_scores_at_minus_infinity(name, make):
+    """Every head's first keys, its last ones, all but one, and all of them (zeros)."""
+    inf = float("inf")
+    for which in ("first", "last", "all_but_one", "all"):
+        c = make()
+        c.p.scale = 0.125
+        n0 = c.ctx if c.prefix else 0
+        n = c.own + n0 if c.prefix else c.ctx
+        left = {"first": range(n // 2, n), "last": range(0, max(1, n // 3)), "all_but_one": range(n // 2, n // 2 + 1), "all": range(0)}[which]
+        for q in c.q:
+            q.zero_()
+            q[..., 0] = 8.0
+        lists = [((c.k[i], c.v[i]), n0) for i in range(c.tiles)] + ([((c.pk, c.pv), 0)] if c.prefix else [])
+        for (k, v), base in lists:
+            at = torch.arange(k.shape[1], device="cuda") + base
+            k.zero_()
+            k[..., 0] = torch.where((at >= left.start) & (at < left.stop), 0.0, -inf).to(k.dtype)
+            v[:] = (at % 5 + 1)[:, None].to(v.dtype)
+        out = c()
+        torch.cuda.synchronize()
+        want = 0.0 if which == "all" else sum(m % 5 + 1 for m in left) / len(left)
+        step = 2.0 ** -8 if c.dtype == "bf16" else 2.0 ** -24
+        for o in out:
+            assert float((o.double() - want).abs().max()) <= (step + (n + 64) * 2.0 ** -24) * want, which
