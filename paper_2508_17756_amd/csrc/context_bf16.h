@@ -1,7 +1,7 @@
-// Shared by the two bf16 kernels of context attention (context_bf16_wide.hip, context_bf16_split.hip): the layout of keys and values in LDS,
-// the fragments read from it, masks, and the transfers that fill it.
+// Shared by the bf16 kernels of context attention (context_bf16_wide.hip, context_bf16_split.hip, context_bf16_resident.hip): the layout of keys
+// and values in LDS, the fragments read from it, masks, and the transfers that fill it.
 //
-// Both kernels form S^T = K Q^T, which puts one row (query) per lane column, so that the probabilities of a row stay in their lanes
+// All of them form S^T = K Q^T, which puts one row (query) per lane column, so that the probabilities of a row stay in their lanes
 // and are already the B operand of O^T = V^T P^T; V^T comes out of LDS through the transposing read.
 #pragma once
 #include "context_common.h"
@@ -69,26 +69,6 @@ __device__ __forceinline__ void load_query(const CtxArgs& a, const CtxTable& tab
   for (int kk = 0; kk < D / 16; ++kk) qf[kk] = __builtin_bit_cast(bf16x8, *(const u32x4*)(q + 16 * kk + 8 * half));
 }
 
-// The keys of one segment as a stage of 64 (or 32) is taken from them.
-struct Segment {
-  const char* k;    // head's first key
-  const char* v;
-  uint32_t token;   // bytes between keys
-  int len;
-  const uint8_t* mask;
-};
-__device__ __forceinline__ Segment segment(const CtxArgs& a, const CtxTable& tab, int which, int tile, int kvh) {
-  Segment g;
-  const void* const k = which == 0 ? a.k0 : tab.k[tile];
-  const void* const v = which == 0 ? a.v0 : tab.v[tile];
-  const int64_t head = (int64_t)kvh * a.kv_head[which] * 2;
-  g.k = (const char*)k + head;
-  g.v = (const char*)v + head;
-  g.token = (uint32_t)(a.kv_token[which] * 2);
-  g.len = which == 0 ? ctx_length(a.len0, 0, a.cap0) : ctx_length(a.len1, tile, a.cap1);
-  g.mask = (which == 1 && a.mask1) ? a.mask1 + (int64_t)tile * a.cap1 : nullptr;
-  return g;
-}
 // Transfers of a wavefront: instruction u moves the slots first + 4 u .. + 3; lane l fills chunk l & 15 of the (l >> 4)-th of them and
 // so fetches the chunk that belongs there: chunk `chunk` of the key `key` behind the first key of these slots.
 template <int D>

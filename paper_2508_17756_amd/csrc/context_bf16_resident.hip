@@ -40,11 +40,11 @@ __global__ __launch_bounds__(kThreads, 2) void context_bf16_resident_kernel(cons
     const int stop = (end < base + p.row_blocks ? end : base + p.row_blocks) - base;   // behind the last row block of this tile and head
     const int nth = pair / a.kv_heads, kvh = __builtin_amdgcn_readfirstlane(pair - nth * a.kv_heads);
     const int tile = __builtin_amdgcn_readfirstlane(ctx_nth_tile(active, nth));
-    const Segment g0 = segment(a, tab, 0, tile, kvh), g1 = segment(a, tab, 1, tile, kvh);
+    const CtxSegment g0 = ctx_segment<2>(a, tab, 0, tile, kvh), g1 = ctx_segment<2>(a, tab, 1, tile, kvh);
     const int n0 = p.seg0 ? (g0.len + 63) / 64 : 0, n = n0 + (p.seg1 ? (g1.len + 63) / 64 : 0);
     // which keys of a unit count
     auto counting = [&](int u) SG_INLINE -> uint64_t {
-      const Segment& g = u >= n0 ? g1 : g0;
+      const CtxSegment& g = u >= n0 ? g1 : g0;
       const int key = (u >= n0 ? u - n0 : u) * 64 + lane;
       bool on = key < g.len;
       if (g.mask && on) on = g.mask[key] != 0;
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kThreads, 2) void context_bf16_resident_kernel(cons
     __syncthreads();   // the keys before these have been attended
     for (int i = wave; i < 2 * n; i += kWaves) {
       const int u = i >> 1;
-      const Segment& g = u >= n0 ? g1 : g0;
+      const CtxSegment& g = u >= n0 ? g1 : g0;
       move_half<D, D / 8>((i & 1) ? g.v : g.k, g.token, (u >= n0 ? u - n0 : u) * 64, 0, counting(u), (i & 1) != 0, lds0 + i * kUnit<D>);
     }
     if (rb < stop) to = rows(rb, qf);

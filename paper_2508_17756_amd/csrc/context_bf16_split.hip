@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArg
   clear(st);
   CtxRowEnd end = {0, 0};   // of row lq
   if (row0 < p.rows) {
-    const Segment g0 = segment(a, tab, 0, batch, kvh), g1 = segment(a, tab, 1, batch, kvh);
+    const CtxSegment g0 = ctx_segment<2>(a, tab, 0, batch, kvh), g1 = ctx_segment<2>(a, tab, 1, batch, kvh);
     const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
     const int n = n0 + n1;
     const int from = (int)((int64_t)n * split / p.splits), to = (int)((int64_t)n * (split + 1) / p.splits);
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256, 1) void context_bf16_split_kernel(const CtxArg
     uint64_t valid_next = 0;
     auto issue = [&](int j, int at) SG_INLINE {
       const bool second = j >= n0;
-      const Segment& g = second ? g1 : g0;
+      const CtxSegment& g = second ? g1 : g0;
       const int key0 = (second ? j - n0 : j) * kKeys;
       bool counts = lane < kKeys && key0 + lane < g.len;
       if (g.mask && counts) counts = g.mask[key0 + lane] != 0;

@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256 * WAYS, 2) void context_bf16_wide_kernel(const 
   const int split = __builtin_amdgcn_readfirstlane(in_head / p.row_blocks), row_block = in_head - split * p.row_blocks;
   const int row0 = row_block * 128 + wave * 32;
 
-  const Segment g0 = segment(a, tab, 0, tile, kvh), g1 = segment(a, tab, 1, tile, kvh);
+  const CtxSegment g0 = ctx_segment<2>(a, tab, 0, tile, kvh), g1 = ctx_segment<2>(a, tab, 1, tile, kvh);
   const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
   const int part = split * WAYS + way, parts = p.splits * WAYS;
   const int from = (int)((int64_t)(n0 + n1) * part / parts), n = (int)((int64_t)(n0 + n1) * (part + 1) / parts) - from;   // stages: j = 0 is `from`
@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256 * WAYS, 2) void context_bf16_wide_kernel(const 
   const int first = wave * (kWideSlots<D> / 4);
   auto request = [&](int j, uint64_t v, bool is_v) SG_INLINE {
     const bool second = from + j >= n0;
-    const Segment& g = second ? g1 : g0;
+    const CtxSegment& g = second ? g1 : g0;
     const int key0 = (second ? from + j - n0 : from + j) * kKeys;
     const uint32_t dst = lds0 + (is_v ? 2 * kHalf : 0) + (j & 1) * kHalf + first * kSlot;
     // (masked keys inside the segment may come along, their scores are replaced; masked values may not: 0 times a NaN is a NaN)

@@ -7,8 +7,9 @@
 // its context).  The group = heads / kv_heads query heads that read the same keys are stacked: a "row" is a (head of the group, token)
 // pair of one tile and one head of keys, rows = group * tokens of them, so that grouped heads fill the tiles of the matrix instruction.
 //
-// A key that does not count (at or behind the segment's length, or masked) has its score set to -inf, and its key and value rows
-// are never read: the transfer takes zeros in their place, so that a NaN or an infinity there does not become 0 * inf.
+// A key that does not count (at or behind the segment's length, or masked) has its score set to -inf.  Its value row is never read: the transfer
+// takes zeros in its place, so that a NaN or an infinity there does not become 0 * inf; nor is its key row, but for masked keys inside
+// the length in the bf16 kernel of shared stages, which come along with the others (a score that is replaced may be anything).
 // A row without any key ends with a sum of 0 and gives zeros.
 #pragma once
 #include "attention_common.h"
@@ -61,6 +62,27 @@ __device__ __forceinline__ int ctx_length(const int32_t* len, int i, int cap) {
   if (!len) return cap;
   const int n = len[i];
   return n < 0 ? 0 : (n > cap ? cap : n);
+}
+// The keys of one segment, of one tile and head of keys, as stages are taken from them; BYTES: of an element.
+struct CtxSegment {
+  const char* k;    // head's first key
+  const char* v;
+  uint32_t token;   // bytes between keys
+  int len;
+  const uint8_t* mask;
+};
+template <int BYTES>
+__device__ __forceinline__ CtxSegment ctx_segment(const CtxArgs& a, const CtxTable& tab, int which, int tile, int kvh) {
+  CtxSegment g;
+  const void* const k = which == 0 ? a.k0 : tab.k[tile];
+  const void* const v = which == 0 ? a.v0 : tab.v[tile];
+  const int64_t head = (int64_t)kvh * a.kv_head[which] * BYTES;
+  g.k = (const char*)k + head;
+  g.v = (const char*)v + head;
+  g.token = (uint32_t)(a.kv_token[which] * BYTES);
+  g.len = which == 0 ? ctx_length(a.len0, 0, a.cap0) : ctx_length(a.len1, tile, a.cap1);
+  g.mask = (which == 1 && a.mask1) ? a.mask1 + (int64_t)tile * a.cap1 : nullptr;
+  return g;
 }
 // Workgroups are dealt round-robin to the 8 XCDs; renumbered so that each XCD walks a contiguous range of the work and what reads the
 // same keys shares one L2.  -1: nothing left.

@@ -25,26 +25,6 @@ namespace {
 constexpr int kHalfStage = 8192, kStage = 2 * kHalfStage, kWaveLds = 2 * kStage, kLds = 4 * kWaveLds;
 constexpr int kSumsAt = kStage, kRowsAt = kSumsAt + 512;
 
-struct Segment {
-  const char* k;
-  const char* v;
-  uint32_t token;
-  int len;
-  const uint8_t* mask;
-};
-__device__ __forceinline__ Segment segment(const CtxArgs& a, const CtxTable& tab, int which, int tile, int kvh) {
-  Segment g;
-  const void* const k = which == 0 ? a.k0 : tab.k[tile];
-  const void* const v = which == 0 ? a.v0 : tab.v[tile];
-  const int64_t head = (int64_t)kvh * a.kv_head[which] * 4;
-  g.k = (const char*)k + head;
-  g.v = (const char*)v + head;
-  g.token = (uint32_t)(a.kv_token[which] * 4);
-  g.len = which == 0 ? ctx_length(a.len0, 0, a.cap0) : ctx_length(a.len1, tile, a.cap1);
-  g.mask = (which == 1 && a.mask1) ? a.mask1 + (int64_t)tile * a.cap1 : nullptr;
-  return g;
-}
-
 // max / sum over the four lane groups
 __device__ __forceinline__ float group_max(float x) {
   const uint32_t u = __float_as_uint(x);
@@ -106,7 +86,7 @@ __global__ __launch_bounds__(256, SHARED ? 3 : 1) void context_f32_kernel(const 
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) end[qb] = {0, 0};
   if (SHARED || row0 < p.rows) {
-    const Segment g0 = segment(a, tab, 0, batch, kvh), g1 = segment(a, tab, 1, batch, kvh);
+    const CtxSegment g0 = ctx_segment<4>(a, tab, 0, batch, kvh), g1 = ctx_segment<4>(a, tab, 1, batch, kvh);
     const int n0 = p.seg0 ? (g0.len + kKeys - 1) / kKeys : 0, n1 = p.seg1 ? (g1.len + kKeys - 1) / kKeys : 0;
     const int n = n0 + n1;
     const int from = (int)((int64_t)n * split / p.splits), to = (int)((int64_t)n * (split + 1) / p.splits);
@@ -116,7 +96,7 @@ __global__ __launch_bounds__(256, SHARED ? 3 : 1) void context_f32_kernel(const 
     // are read along and stay as they are
     auto issue = [&](int j, int at) SG_INLINE {
       const bool second = j >= n0;
-      const Segment& g = second ? g1 : g0;
+      const CtxSegment& g = second ? g1 : g0;
       const int key0 = (second ? j - n0 : j) * kKeys;
       bool counts = lane < kKeys && key0 + lane < g.len;
       if (g.mask && counts) counts = g.mask[key0 + lane] != 0;
