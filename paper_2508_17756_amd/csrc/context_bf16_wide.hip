@@ -33,16 +33,9 @@ __global__ __launch_bounds__(256 * WAYS, 2) void context_bf16_wide_kernel(const 
   const uint32_t lds_all = (uint32_t)(uintptr_t)(SG_LDS uint8_t*)smem, lds0 = lds_all + way * kWideLds<D>;
   const int lq = lane & 31, half = lane >> 5;
   const CtxPart& p = a.part;
-  // Only the tiles that run are numbered, so that the work is spread evenly whichever they are.
-  uint64_t active = p.stacked ? 1 : a.n_tiles >= 64 ? ~0ull : (1ull << a.n_tiles) - 1;
-  if (a.run && !p.stacked) active = __ballot(lane < a.n_tiles && a.run[lane < a.n_tiles ? lane : 0] != 0);
-  const int per_head = p.splits * p.row_blocks, per_tile = a.kv_heads * per_head;
-  const int id = ctx_xcd_order((int)blockIdx.x, __builtin_popcountll(active) * per_tile);
-  if (id < 0) return;
-  const int nth = id / per_tile, in_tile = id - nth * per_tile;
-  const int tile = __builtin_amdgcn_readfirstlane(ctx_nth_tile(active, nth));
-  const int kvh = __builtin_amdgcn_readfirstlane(in_tile / per_head), in_head = in_tile - kvh * per_head;
-  const int split = __builtin_amdgcn_readfirstlane(in_head / p.row_blocks), row_block = in_head - split * p.row_blocks;
+  CtxItem item;
+  if (!ctx_shared_item(a, p, item)) return;
+  const int tile = item.tile, kvh = item.kvh, split = item.split, row_block = item.row_block;
   const int row0 = row_block * 128 + wave * 32;
 
   const CtxSegment g0 = ctx_segment<2>(a, tab, 0, tile, kvh), g1 = ctx_segment<2>(a, tab, 1, tile, kvh);

@@ -96,6 +96,27 @@ __device__ __forceinline__ int ctx_nth_tile(uint64_t mask, int a) {
   return __builtin_ctzll(mask);
 }
 
+// What a workgroup of the kernels with shared stages takes.  Only the tiles that run are numbered, so that the work is spread evenly whichever they
+// are and the rest of the grid exits at once.  False: nothing.
+struct CtxItem {
+  int tile, kvh, split, row_block;
+};
+__device__ __forceinline__ bool ctx_shared_item(const CtxArgs& a, const CtxPart& p, CtxItem& item) {
+  const int lane = threadIdx.x & 63;
+  uint64_t active = p.stacked ? 1 : a.n_tiles >= 64 ? ~0ull : (1ull << a.n_tiles) - 1;
+  if (a.run && !p.stacked) active = __ballot(lane < a.n_tiles && a.run[lane < a.n_tiles ? lane : 0] != 0);
+  const int per_head = p.splits * p.row_blocks, per_tile = a.kv_heads * per_head;
+  const int id = ctx_xcd_order((int)blockIdx.x, __builtin_popcountll(active) * per_tile);
+  if (id < 0) return false;
+  const int nth = id / per_tile, in_tile = id - nth * per_tile;
+  item.tile = __builtin_amdgcn_readfirstlane(ctx_nth_tile(active, nth));
+  item.kvh = __builtin_amdgcn_readfirstlane(in_tile / per_head);
+  const int in_head = in_tile - item.kvh * per_head;
+  item.split = __builtin_amdgcn_readfirstlane(in_head / p.row_blocks);
+  item.row_block = in_head - item.split * p.row_blocks;
+  return true;
+}
+
 struct CtxRow {
   int tile, head, token;   // head: of the queries
   int rid;                 // row among the launch's rows: its place in the workspace

@@ -54,21 +54,19 @@ __global__ __launch_bounds__(256, SHARED ? 3 : 1) void context_f32_kernel(const 
   const CtxPart& p = a.part;
   int split, row_block, kvh, batch;
   if constexpr (SHARED) {
-    int id = ctx_xcd_order((int)blockIdx.x, p.items);
-    if (id < 0) return;
-    row_block = id % p.row_blocks;
-    id /= p.row_blocks;
-    split = id % p.splits;
-    id /= p.splits;
-    kvh = id % a.kv_heads;
-    batch = id / a.kv_heads;
+    CtxItem item;
+    if (!ctx_shared_item(a, p, item)) return;
+    batch = item.tile;
+    kvh = item.kvh;
+    split = item.split;
+    row_block = item.row_block;
   } else {   // the grid names tile and head of keys, so that the table of tiles can be read without waiting for anything else
     split = (int)blockIdx.x / p.row_blocks;
     row_block = (int)blockIdx.x - split * p.row_blocks;
     kvh = (int)blockIdx.y;
     batch = (int)blockIdx.z;
+    if (!p.stacked && a.run && a.run[batch] == 0) return;
   }
-  if (!p.stacked && a.run && a.run[batch] == 0) return;
   const int way = wave & (p.ways - 1);
   const int row0 = (row_block * (4 / p.ways) + wave / p.ways) * kRows;
   const uint32_t mine = SHARED ? lds0 : lds0 + wave * kWaveLds;
