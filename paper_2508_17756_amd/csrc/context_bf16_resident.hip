@@ -3,9 +3,11 @@
 //
 // A workgroup of 8 wavefronts, one per compute unit, takes a run of row blocks (32 rows each) from the list of all of them; where the run enters
 // another tile or head of keys the keys are exchanged.  Between two exchanges the wavefronts go their own ways, a row block each, without
-// barriers and without transfers: rows in, all keys, rows out; the next block's rows are requested before this one's keys are attended.  Bound by
-// the vector ALU (exponentials) first, the rows' traffic next: 4 tiles of 17,550 rows, 48 heads x 64, 226 keys 0.36 ms (2.4 TB/s, 0.54 PFLOP/s; with
-// shared stages 0.41), 4 x 9,000 rows, 24 heads x 128, 256 keys 0.16 ms (2.8 TB/s; 0.18).  12 wavefronts a compute unit gain nothing, 16 spill.
+// barriers and without transfers: rows in, all keys, rows out; the next block's rows are requested before this one's keys are attended.  No unit is
+// busy all the time (vector ALU 60 % of the cycles, exponentials first, matrix pipe 26 %, LDS 15 %): products and softmax of a row block follow one
+// another, and the two wavefronts of a SIMD hide part of each other.  4 tiles of 17,550 rows, 48 heads x 64, 226 keys 0.35 - 0.38 ms from device to
+// device (2.3 - 2.5 TB/s, 0.51 - 0.56 PFLOP/s; with shared stages 0.41 where this took 0.36), 4 x 9,000 rows, 24 heads x 128, 256 keys 0.16 ms
+// (2.8 TB/s; 0.18).  12 wavefronts a compute unit gain nothing, 16 spill.
 #include <atomic>
 #include "context_bf16.h"
 

@@ -1,8 +1,8 @@
 // Context attention (sg_tile_cross_attention, sg_tile_prefix_attention) of calls with few rows, bf16: every wavefront streams keys of its own
 // through LDS of its own, 32 rows at a time, and the shares of a row are joined in LDS and, over workgroups, by the join kernel.
 //
-// Bound by latency: a wavefront waits for nobody but its own transfers.  One token of 8 heads x 64 over 77 keys 6.9 us, a launch that does nothing
-// about 5; 20 single tokens' own keys (up to 460, 8 heads of keys x 128) and the join of 32 shares of a prefix 14 us.
+// Bound by latency: a wavefront waits for nobody but its own transfers.  One token of 8 heads x 64 over 77 keys 6.7 - 7.2 us, of one
+// head over one key 7.0 (6.1 between the kernel's begin and end); 20 single tokens' own keys (up to 460, 8 heads of keys x 128) and the join of 32 shares of a prefix 14 us.
 #include <atomic>
 #include "context_bf16.h"
 

@@ -6,9 +6,10 @@
 // of stage j on the vector ALU between the products of its neighbours, PV of stage j - 1 and QK of stage j + 1, on the matrix pipe.  Two
 // workgroups run beside one another on a compute unit, so that the start and the end of one (rows in, rows out) hide behind the other.
 //
-// Measured: 9 tiles of 3,840 rows over 512 + 3,840 keys, 24 heads x 128, 1.80 ms = 1.03 PFLOP/s at 1.8 GHz (power), matrix pipe 51 % busy; without
-// transfers the loop takes 1.53 ms, without the fragment reads 1.36, without both 1.08: bound by waits for LDS.  8 stages (75,600 rows over 512 keys,
-// 40 heads) 0.96 ms = 0.82 PFLOP/s: start and end.  head_dim 64 (48 heads, 4 x 2,925 rows over 226 + 2,925 keys) 0.59 ms = 0.77: exponentials.
+// Measured, from device to device: 9 tiles of 3,840 rows over 512 + 3,840 keys, 24 heads x 128, 1.74 - 1.91 ms = 0.97 - 1.06 PFLOP/s at 1.74 - 1.83 GHz
+// (power), matrix pipe 51 - 53 % busy; where it took 1.80, the loop took 1.53 ms without transfers, 1.36 without the fragment reads, 1.08 without both: bound
+// by waits for LDS.  8 stages (75,600 rows over 512 keys, 40 heads) 0.93 - 1.03 ms = 0.77 - 0.85 PFLOP/s: start and end.  head_dim 64 (48 heads,
+// 4 x 2,925 rows over 226 + 2,925 keys) 0.57 - 0.62 ms = 0.73 - 0.80: exponentials.
 #include <atomic>
 #include <type_traits>
 #include "context_bf16.h"
