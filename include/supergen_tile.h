@@ -526,9 +526,9 @@ typedef struct sg_norm_problem {
  *   weight     device, `channels` elements, or NULL: ones
  *   sum        host array: s in the tensors' type, or NULL.  sum[i] may be x[i] or residual[i] (with its stride): in place.  No other tile may have
  *              that buffer as x, residual or sum (tiles that do not write in place may share x and residual)
- *   out        host array: y in the tensors' type; or, with SG_F8_E4M3, y / scale rounded to 8 bits, scale = max|y| / 448 over a
- *              row or over each 128 channels of it (0 where that maximum is below 2^-100: zeros are written; NaN, as all 8-bit values of the row
- *              or block, where one of them is).  Aliases nothing
+ *   out        host array: y in the tensors' type; or, with SG_F8_E4M3, y * (448 / max|y|) rounded to 8 bits, scale = max|y| / 448, the maximum over a
+ *              row or over each 128 channels of it (below 2^-100: zeros and a scale of 0 are written; where one of its y is NaN, NaN for all of
+ *              them and the scale).  Aliases nothing
  *   out_scale  SG_F8_E4M3: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats; else NULL
  *   run        device, n_tiles bytes, or NULL: all tiles
  * y is computed from the sum before it is rounded, in fp32, for every finite s: where the sum of the squares would leave the fp32 range, it is taken
