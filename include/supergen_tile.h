@@ -13,7 +13,8 @@
  *                           input (Equation 3) against a threshold (Equation 7)
  *   sg_denoise_step_tiled   one stage-2 step: gate -> attention on the tiles to recompute ->
  *                           cache refresh -> Fuse (Algorithm 1 loop body; Section 5.1 pipeline)
- *   sg_tile_cross_attention, sg_tile_prefix_attention, sg_tile_residual_norm
+ *   sg_tile_cross_attention, sg_tile_prefix_attention, sg_tile_residual_norm,
+ *   sg_tile_rotary, sg_tile_gated_norm, sg_tile_int8_linear
  *                           what the transformer block of a tile has beside its self-attention
  *
  * Conventions shared by every entry point
@@ -58,7 +59,8 @@ extern "C" {
 typedef enum {
   SG_F32 = 0,
   SG_BF16 = 1,
-  SG_F8_E4M3 = 2 /* 8 bits, 4 of exponent, 3 of mantissa, largest 448, no infinity: an output of sg_tile_residual_norm */
+  SG_F8_E4M3 = 2, /* 8 bits, 4 of exponent, 3 of mantissa, largest 448, no infinity: an output of the norms */
+  SG_I8 = 3       /* 8-bit integers -127 .. 127: an output of sg_tile_gated_norm                               */
 } sg_dtype;
 
 typedef enum {
@@ -538,6 +540,140 @@ typedef struct sg_norm_problem {
 int sg_tile_residual_norm(const sg_norm_problem* p, int32_t n_tiles, const void* const* x, const void* const* residual,
                           const void* weight, const uint8_t* run, void* const* sum, void* const* out,
                           float* const* out_scale, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Rotary positions: pairs of a head's channels are turned by angles that grow with the token's place, so that scores of attention depend on
+ * distances.  The first R = axis_t + axis_y + axis_x channels of a head turn, the others pass as they are.  Pair i < R / 2 is
+ *     SG_ROTARY_INTERLEAVED   channels (2 i, 2 i + 1)          SG_ROTARY_HALF   channels (i, i + R / 2)
+ * and the pairs belong to the axes in their order: the first axis_t / 2 to t, then y, then x.  A pair (a, b) becomes
+ *     (a cos w - b sin w, b cos w + a sin w),   w = frequency[i] * (the token's position on the pair's axis).
+ * Token n of a tile is (t, y, x) = (n / (H W), n / W mod H, n mod W). */
+typedef enum { SG_ROTARY_INTERLEAVED = 0, SG_ROTARY_HALF = 1 } sg_rotary_layout;
+
+/* How positions beyond those a model was trained on are brought back (sg_rotary_frequencies). */
+typedef enum { SG_ROTARY_PLAIN = 0, SG_ROTARY_LINEAR = 1, SG_ROTARY_NTK = 2, SG_ROTARY_RAMP = 3 } sg_rotary_scaling;
+
+typedef struct sg_rotary_problem {
+  int32_t T, H, W;            /* tokens of a tile: T * H * W >= 1, below 2^24                                     */
+  int32_t heads, kv_heads;    /* heads of q and of k, 1 .. 65535 (kv_heads is not looked at without k)            */
+  int32_t head_dim;           /* a multiple of 8, 8 .. 512                                                       */
+  int32_t dtype;              /* SG_F32 or SG_BF16, of every tensor and weight                                   */
+  int32_t layout;             /* sg_rotary_layout                                                                */
+  int32_t axis_t, axis_y, axis_x;          /* channels that turn with each axis: even, >= 0, R >= 2; SG_ROTARY_HALF: R a multiple of 16 */
+  int32_t canvas_t, canvas_h, canvas_w;    /* with origins: positions wrap around at this size; 0: they do not   */
+  int32_t position_axes;      /* listed positions: 1 (one number a token, of every axis) or 3 (t, y, x)          */
+  float eps;                  /* of the norm of a head, >= 0                                                     */
+  int64_t q_stride_token, q_stride_head, q_out_stride_token, q_out_stride_head;   /* as in sg_context_problem    */
+  int64_t k_stride_token, k_stride_head, k_out_stride_token, k_out_stride_head;
+} sg_rotary_problem;
+
+/* Checks a rotary problem (host only, launches nothing). */
+int sg_rotary_validate(const sg_rotary_problem* p);
+
+/*
+ * Frequencies of the R / 2 pairs in radians per position (host only; `out` is host memory, what sg_tile_rotary reads a device copy of it):
+ * base^(-2 i / n) for pair i of an axis of n channels, and then
+ *   SG_ROTARY_LINEAR   divided by factor
+ *   SG_ROTARY_NTK      of base * factor^(n / (n - 2)) in the place of base: the last pair of an axis is divided by factor, the first stays
+ *   SG_ROTARY_RAMP     pairs that turn `fast` times or more over `length` positions stay, those that turn `slow` times or less are divided by factor,
+ *                      and between them the part that stays grows in proportion
+ * base > 0, factor > 0, length > 0, 0 <= slow < fast, all finite (factor, length, slow, fast: where the scaling uses them).
+ */
+int sg_rotary_frequencies(const sg_rotary_problem* p, double base, int32_t scaling, double factor, double length, double slow, double fast,
+                          double* out);
+
+/*
+ * Turns the queries of tiles, and their keys in the same pass.
+ *   q, q_out     host arrays of n_tiles device pointers.  q_out[i] may be q[i] (with its strides): in place.  No other tile may have that buffer
+ *   k, k_out     the same of the keys, or both NULL
+ *   frequencies  device, R / 2 doubles (8-byte aligned)
+ *   origin       host, [n_tiles][3] int32: position (t, y, x) of tile i's first token; token (t, y, x) of the tile sits at origin + (t, y, x), modulo
+ *                the canvas on the axes that have one.  Any numbers, on axes without a canvas such that the sums stay inside 32 bits.  They travel with the launch: a captured call keeps them
+ *   positions    host array of n_tiles device pointers to [tokens][position_axes] int32 (any values), instead of origin; canvas sizes are not looked at
+ *   q_weight, k_weight  device, head_dim elements, or NULL.  Where one is given, that tensor's heads are first normalised:
+ *                x * rsqrt(mean(x^2) + eps) * weight over the head_dim channels, fp32
+ *   run          device, n_tiles bytes, or NULL: all tiles
+ * Exactly one of origin and positions.  Angles are products in fp64, reduced to one turn before they are rounded to fp32; sine and cosine are good to
+ * 2^-21 for positions below 2^27 in size; everything else is fp32, rounded once.  Channels behind R pass bit by bit where there is no norm (NaN may change its payload).
+ * Tensors are 16-byte aligned.
+ */
+int sg_tile_rotary(const sg_rotary_problem* p, int32_t n_tiles, const void* const* q, const void* const* k, const double* frequencies,
+                   const int32_t* origin, const int32_t* const* positions, const void* q_weight, const void* k_weight, const uint8_t* run,
+                   void* const* q_out, void* const* k_out, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The norms of a block: the one behind a sublayer, its gate, the residual stream, the one before the next sublayer and its modulation, in one pass. */
+typedef enum { SG_NORM_NONE = 0, SG_NORM_RMS = 1, SG_NORM_LAYER = 2 } sg_norm_kind;
+
+/* Shapes: rows x channels per tile; row n of a tensor begins at base + n*stride (elements). */
+typedef struct sg_gated_norm_problem {
+  int32_t rows;               /* per tile, >= 0                                                                  */
+  int32_t channels;           /* a multiple of 8, 8 .. 32768                                                     */
+  int32_t dtype;              /* SG_F32 or SG_BF16: x, residual, weights, sum                                     */
+  int32_t out_dtype;          /* dtype, SG_F8_E4M3 or SG_I8                                                       */
+  int32_t scale_group;        /* 8 bits: channels that share a scale: 0 = the whole row, or 128 (a divisor of channels) */
+  int32_t norm;               /* SG_NORM_RMS or SG_NORM_LAYER, before the next sublayer                          */
+  int32_t post_norm;          /* sg_norm_kind, behind the last one                                               */
+  int32_t mod_dtype;          /* dtype or SG_F32: gate, scale, shift                                              */
+  int32_t mod_rows;           /* rows that share a vector of gate, scale and shift: row n has vector n / mod_rows; 0: all rows of the tile */
+  float residual_scale;       /* finite                                                                          */
+  float eps, post_eps;        /* >= 0                                                                            */
+  int64_t x_stride, residual_stride, sum_stride, out_stride;   /* multiples of 8, >= channels                     */
+  int64_t mod_stride;         /* between the vectors of a tile: a multiple of 8, >= channels (one vector: not looked at) */
+} sg_gated_norm_problem;
+
+/*
+ * Per row:   s = residual_scale * residual + gate * post(x) * post_weight,      y = norm(s) * weight * (1 + scale) + shift
+ *   post, norm   SG_NORM_RMS: v * rsqrt(mean(v^2) + eps);  SG_NORM_LAYER: (v - mean(v)) * rsqrt(mean((v - mean(v))^2) + eps);  SG_NORM_NONE: v
+ *   residual     host array of n_tiles device pointers, or NULL: 0 (and residual_scale is not looked at)
+ *   gate, scale, shift   host arrays of device pointers to [vectors][channels], each or NULL: 1, 0, 0
+ *   post_weight, weight  device, `channels` elements, or NULL: ones (post_weight: only with a post_norm)
+ *   sum          host array: s in the tensors' type, or NULL.  sum[i] may be x[i] or residual[i] as in sg_tile_residual_norm
+ *   out          host array: y in the tensors' type; or in 8 bits, y * (M / max|y|) rounded to the nearest (ties to even), out_scale = max|y| / M, with
+ *                M = 448 (SG_F8_E4M3) or 127 (SG_I8), the maximum over a row or over each 128 channels of it; below 2^-100: zeros and a scale of 0;
+ *                where one of its y is NaN or infinite the scale is NaN (and so is what the 8 bits stand for).  Aliases nothing
+ *   out_scale    8 bits: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats; else NULL
+ *   run          device, n_tiles bytes, or NULL: all tiles
+ * Everything is fp32 between the loads and the stores: y comes from the sum before it is rounded, for every finite s, as in sg_tile_residual_norm; the
+ * mean of SG_NORM_LAYER is taken twice, the second time of what the first leaves, so that rows far from 0 keep their digits.  With eps = 0 a row of zeros
+ * (SG_NORM_LAYER: of one value) gives NaN.  A row with a NaN is NaN throughout, and so is one with an infinity behind SG_NORM_LAYER (SG_NORM_RMS: NaN there, 0
+ * elsewhere).  All pointers 16-byte aligned (out_scale: 4).
+ */
+int sg_tile_gated_norm(const sg_gated_norm_problem* p, int32_t n_tiles, const void* const* x, const void* const* residual, const void* const* gate,
+                       const void* post_weight, const void* weight, const void* const* scale, const void* const* shift, const uint8_t* run,
+                       void* const* sum, void* const* out, float* const* out_scale, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Linear layer in 8-bit integers: a scale for each token and one for each output. */
+typedef enum { SG_ACT_NONE = 0, SG_ACT_GELU = 1 } sg_activation;
+
+typedef struct sg_int8_linear_problem {
+  int32_t rows;               /* tokens of a tile, >= 0                                                          */
+  int32_t channels;           /* inputs: a multiple of 16, 16 .. 131056                                          */
+  int32_t outputs;            /* a multiple of 8, >= 8                                                           */
+  int32_t dtype;              /* SG_F32 or SG_BF16: bias and out                                                  */
+  int32_t activation;         /* sg_activation                                                                   */
+  int64_t x_stride, w_stride; /* between rows, in elements: multiples of 16, >= channels                         */
+  int64_t out_stride;         /* a multiple of 8, >= outputs                                                     */
+} sg_int8_linear_problem;
+
+/* Checks a linear problem (host only, launches nothing). */
+int sg_int8_linear_validate(const sg_int8_linear_problem* p);
+
+/*
+ * For row n of tile i and output o:   v = x_scale[i][n] * w_scale[o] * sum_c x[i][n][c] * w[o][c] + bias[o],   out = v or GELU(v)
+ *   x          host array of n_tiles device pointers to rows of 8-bit integers (what sg_tile_gated_norm leaves with SG_I8 and scale_group 0)
+ *   x_scale    host array of device pointers to [rows] floats;  w_scale: device, `outputs` floats
+ *   w          device, [outputs][channels] 8-bit integers
+ *   bias       device, `outputs` elements of dtype, or NULL: 0
+ *   run        device, n_tiles bytes, or NULL: all tiles
+ *   out        host array of device pointers: rows of outputs in dtype; alias nothing
+ * The sum is one of integers in 32 bits and exact (-128 too); it is rounded to fp32 and scaled there, first by the token's, then by the output's factor, and the
+ * result is rounded once.  GELU is v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2.  A token or output whose scale is NaN gives NaN, and no other does.
+ * Tensors are 16-byte aligned (x_scale: 4).  rows * n_tiles is below 2^31, rows * outputs of 64 tiles below 2^39.
+ */
+int sg_tile_int8_linear(const sg_int8_linear_problem* p, int32_t n_tiles, const void* const* x, const float* const* x_scale, const void* w,
+                        const float* w_scale, const void* bias, const uint8_t* run, void* const* out, void* stream);
 
 #ifdef __cplusplus
 }

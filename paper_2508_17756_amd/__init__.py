@@ -10,4 +10,8 @@ from .binding import (  # noqa: F401
     sg_cache_gate_static, SG_STATIC_GATE_MAX_TILES, sg_tile_similarity,
     sg_context_problem, make_context_problem, sg_context_validate, sg_context_workspace_bytes,
     sg_tile_cross_attention, sg_tile_prefix_attention, sg_norm_problem, make_norm_problem, sg_tile_residual_norm,
+    SG_I8, SG_ROTARY_INTERLEAVED, SG_ROTARY_HALF, SG_ROTARY_PLAIN, SG_ROTARY_LINEAR, SG_ROTARY_NTK, SG_ROTARY_RAMP,
+    sg_rotary_problem, make_rotary_problem, sg_rotary_validate, sg_rotary_frequencies, sg_tile_rotary,
+    SG_NORM_NONE, SG_NORM_RMS, SG_NORM_LAYER, sg_gated_norm_problem, make_gated_norm_problem, sg_tile_gated_norm,
+    SG_ACT_NONE, SG_ACT_GELU, sg_int8_linear_problem, make_int8_linear_problem, sg_int8_linear_validate, sg_tile_int8_linear,
 )

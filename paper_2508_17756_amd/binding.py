@@ -8,10 +8,14 @@ been built, loading raises.
 import ctypes
 import os
 
-SG_F32, SG_BF16, SG_F8_E4M3 = 0, 1, 2
+SG_F32, SG_BF16, SG_F8_E4M3, SG_I8 = 0, 1, 2, 3
 SG_OK, SG_ERR_INVALID_ARG, SG_ERR_UNSUPPORTED, SG_ERR_WORKSPACE, SG_ERR_HIP = 0, -1, -2, -3, -4
 SG_REGION_MAXMIN, SG_REGION_TOPSELECT = 0, 1
 SG_STATIC_GATE_MAX_TILES = 64
+SG_ROTARY_INTERLEAVED, SG_ROTARY_HALF = 0, 1
+SG_ROTARY_PLAIN, SG_ROTARY_LINEAR, SG_ROTARY_NTK, SG_ROTARY_RAMP = 0, 1, 2, 3
+SG_NORM_NONE, SG_NORM_RMS, SG_NORM_LAYER = 0, 1, 2
+SG_ACT_NONE, SG_ACT_GELU = 0, 1
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -94,6 +98,33 @@ class sg_norm_problem(ctypes.Structure):
                 ("out_stride", ctypes.c_int64)]
 
 
+class sg_rotary_problem(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("H", ctypes.c_int32), ("W", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("layout", ctypes.c_int32),
+                ("axis_t", ctypes.c_int32), ("axis_y", ctypes.c_int32), ("axis_x", ctypes.c_int32),
+                ("canvas_t", ctypes.c_int32), ("canvas_h", ctypes.c_int32), ("canvas_w", ctypes.c_int32),
+                ("position_axes", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q_stride_token", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("q_out_stride_token", ctypes.c_int64), ("q_out_stride_head", ctypes.c_int64),
+                ("k_stride_token", ctypes.c_int64), ("k_stride_head", ctypes.c_int64),
+                ("k_out_stride_token", ctypes.c_int64), ("k_out_stride_head", ctypes.c_int64)]
+
+
+class sg_gated_norm_problem(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("channels", ctypes.c_int32), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("scale_group", ctypes.c_int32), ("norm", ctypes.c_int32), ("post_norm", ctypes.c_int32), ("mod_dtype", ctypes.c_int32),
+                ("mod_rows", ctypes.c_int32), ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float), ("post_eps", ctypes.c_float),
+                ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("sum_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("mod_stride", ctypes.c_int64)]
+
+
+class sg_int8_linear_problem(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("channels", ctypes.c_int32), ("outputs", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("activation", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
 def library_path():
     return os.path.join(_PKG, "libsupergen_tile.so")
 
@@ -169,6 +200,20 @@ def load_library():
     lib.sg_tile_prefix_attention.argtypes = [ctx, i32, pp, pp, pp, vp, vp, vp, vp, vp, pp, vp, ctypes.c_size_t, vp]
     lib.sg_tile_residual_norm.restype = ctypes.c_int
     lib.sg_tile_residual_norm.argtypes = [ctypes.POINTER(sg_norm_problem), i32, pp, pp, vp, vp, pp, pp, pp, vp]
+    rot = ctypes.POINTER(sg_rotary_problem)
+    lib.sg_rotary_validate.restype = ctypes.c_int
+    lib.sg_rotary_validate.argtypes = [rot]
+    lib.sg_rotary_frequencies.restype = ctypes.c_int
+    lib.sg_rotary_frequencies.argtypes = [rot, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                          ctypes.POINTER(ctypes.c_double)]
+    lib.sg_tile_rotary.restype = ctypes.c_int
+    lib.sg_tile_rotary.argtypes = [rot, i32, pp, pp, vp, ctypes.POINTER(i32), pp, vp, vp, vp, pp, pp, vp]
+    lib.sg_tile_gated_norm.restype = ctypes.c_int
+    lib.sg_tile_gated_norm.argtypes = [ctypes.POINTER(sg_gated_norm_problem), i32, pp, pp, pp, vp, vp, pp, pp, vp, pp, pp, pp, vp]
+    lib.sg_int8_linear_validate.restype = ctypes.c_int
+    lib.sg_int8_linear_validate.argtypes = [ctypes.POINTER(sg_int8_linear_problem)]
+    lib.sg_tile_int8_linear.restype = ctypes.c_int
+    lib.sg_tile_int8_linear.argtypes = [ctypes.POINTER(sg_int8_linear_problem), i32, pp, pp, vp, vp, vp, vp, pp, vp]
     _LIB = lib
     return lib
 
@@ -491,7 +536,8 @@ def sg_region_thresholds(tile_std, track_mean, track_count, tau_base, alpha, mod
 
 
 # ------------------------------------------------------------------ the rest of a tile's block: context attention, residual norm
-_DTYPES = {"f32": SG_F32, "bf16": SG_BF16, "e4m3": SG_F8_E4M3, SG_F32: SG_F32, SG_BF16: SG_BF16, SG_F8_E4M3: SG_F8_E4M3}
+_DTYPES = {"f32": SG_F32, "bf16": SG_BF16, "e4m3": SG_F8_E4M3, "int8": SG_I8, SG_F32: SG_F32, SG_BF16: SG_BF16, SG_F8_E4M3: SG_F8_E4M3,
+           SG_I8: SG_I8}
 
 
 def make_context_problem(tokens, ctx_tokens, heads, head_dim, dtype, kv_heads=None, own_tokens=0, scale=None, token_major=False):
@@ -583,4 +629,110 @@ def sg_tile_residual_norm(p, x, weight, out, residual=None, sum_out=None, out_sc
     st = load_library().sg_tile_residual_norm(ctypes.byref(p), n, _ptr_array(x), _pointers(residual, n), _ptr(weight),
                                               _flags(run, n, "run"), _pointers(sum_out, n), _pointers(out, n), _pointers(out_scale, n), _stream())
     _check(st, "sg_tile_residual_norm")
+    return out
+
+
+# ------------------------------------------------------------------ rotary positions, gated norm, 8-bit integer linear layer
+_LAYOUTS = {"interleaved": SG_ROTARY_INTERLEAVED, "half": SG_ROTARY_HALF}
+_SCALINGS = {"none": SG_ROTARY_PLAIN, "linear": SG_ROTARY_LINEAR, "ntk": SG_ROTARY_NTK, "ramp": SG_ROTARY_RAMP}
+_NORMS = {"none": SG_NORM_NONE, "rms": SG_NORM_RMS, "layer": SG_NORM_LAYER}
+_ACTIVATIONS = {None: SG_ACT_NONE, "none": SG_ACT_NONE, "gelu": SG_ACT_GELU}
+
+
+def make_rotary_problem(size, heads, head_dim, dtype, axes, kv_heads=None, layout="interleaved", wrap=None, eps=1e-6, position_axes=1,
+                        token_major=False):
+    """sg_rotary_problem of packed tensors: [heads][tokens][d], or [tokens][heads][d] if token_major.  Other strides: set the fields.
+    size: (T, H, W) of a tile; axes: channels of a head that turn with t, y and x; wrap: None or the canvas' (T, H, W), 0 where an axis does not wrap."""
+    kv = heads if kv_heads is None else kv_heads
+    t, h, w = (int(n) for n in size)
+    c = (0, 0, 0) if wrap is None else wrap
+    p = sg_rotary_problem(T=t, H=h, W=w, heads=int(heads), kv_heads=int(kv), head_dim=int(head_dim), dtype=_DTYPES[dtype], layout=_LAYOUTS[layout],
+                          axis_t=int(axes[0]), axis_y=int(axes[1]), axis_x=int(axes[2]), canvas_t=int(c[0]), canvas_h=int(c[1]), canvas_w=int(c[2]),
+                          position_axes=int(position_axes), eps=float(eps))
+    for name, a in (("q", heads), ("q_out", heads), ("k", kv), ("k_out", kv)):
+        setattr(p, name + "_stride_token", int(a) * int(head_dim) if token_major else int(head_dim))
+        setattr(p, name + "_stride_head", int(head_dim) if token_major else max(1, t * h * w) * int(head_dim))
+    return p
+
+
+def sg_rotary_validate(p):
+    return load_library().sg_rotary_validate(ctypes.byref(p))
+
+
+def sg_rotary_frequencies(p, base=10000.0, scaling="none", factor=1.0, length=1.0, slow=1.0, fast=32.0, device="cuda"):
+    """Radians per position of every pair, as the float64 tensor on `device` that sg_tile_rotary reads."""
+    n = max(0, (p.axis_t + p.axis_y + p.axis_x) // 2)
+    out = (ctypes.c_double * (n or 1))()
+    _check(load_library().sg_rotary_frequencies(ctypes.byref(p), float(base), _SCALINGS[scaling], float(factor), float(length), float(slow), float(fast),
+                                                out), "sg_rotary_frequencies")
+    torch = _torch()
+    return torch.tensor(list(out)[:n], dtype=torch.float64, device=device)
+
+
+def sg_tile_rotary(p, q, q_out, frequencies, k=None, k_out=None, origin=None, positions=None, q_weight=None, k_weight=None, run=None):
+    """q, q_out, k, k_out: lists of one tensor per tile (k, k_out: or None); frequencies: float64; origin: one (t, y, x) per tile, or positions: lists
+    of one int32 tensor [tokens][p.position_axes] per tile; q_weight, k_weight: head_dim elements or None; run: uint8 or bool."""
+    n, torch = len(q), _torch()
+    pairs = (p.axis_t + p.axis_y + p.axis_x) // 2
+    at = None
+    if origin is not None:
+        if len(origin) != n:
+            raise ValueError("%d origins for %d tiles" % (len(origin), n))
+        at = (ctypes.c_int32 * (3 * n or 1))(*[int(v) for o in origin for v in (o[0], o[1], o[2])])
+    if positions is not None:
+        for t in positions:
+            _vector(t, (torch.int32,), p.T * p.H * p.W * p.position_axes, "positions")
+    st = load_library().sg_tile_rotary(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _vector(frequencies, (torch.float64,), pairs, "frequencies"), at,
+                                       _pointers(positions, n), _ptr(q_weight), _ptr(k_weight), _flags(run, n, "run"), _pointers(q_out, n),
+                                       _pointers(k_out, n), _stream())
+    _check(st, "sg_tile_rotary")
+    return q_out if k is None else (q_out, k_out)
+
+
+def make_gated_norm_problem(rows, channels, dtype, out_dtype=None, scale_group=0, norm="rms", post_norm="none", residual_scale=1.0, mod_rows=0,
+                            mod_dtype=None, eps=1e-6, post_eps=1e-6):
+    """sg_gated_norm_problem of packed rows and vectors; other strides: set the fields.  out_dtype: None (as dtype), "e4m3" or "int8"; mod_dtype: None
+    (as dtype) or "f32"."""
+    c = int(channels)
+    return sg_gated_norm_problem(rows=int(rows), channels=c, dtype=_DTYPES[dtype], out_dtype=_DTYPES[dtype if out_dtype is None else out_dtype],
+                                 scale_group=int(scale_group), norm=_NORMS[norm], post_norm=_NORMS[post_norm],
+                                 mod_dtype=_DTYPES[dtype if mod_dtype is None else mod_dtype], mod_rows=int(mod_rows),
+                                 residual_scale=float(residual_scale), eps=float(eps), post_eps=float(post_eps), x_stride=c, residual_stride=c,
+                                 sum_stride=c, out_stride=c, mod_stride=c)
+
+
+def sg_tile_gated_norm(p, x, out, residual=None, gate=None, post_weight=None, weight=None, scale=None, shift=None, sum_out=None, out_scale=None,
+                       run=None):
+    """x, out, residual, gate, scale, shift, sum_out, out_scale: lists of one tensor per tile, all but the first two or None; post_weight, weight:
+    `channels` elements or None; run: uint8 or bool."""
+    n = len(x)
+    st = load_library().sg_tile_gated_norm(ctypes.byref(p), n, _ptr_array(x), _pointers(residual, n), _pointers(gate, n), _ptr(post_weight),
+                                           _ptr(weight), _pointers(scale, n), _pointers(shift, n), _flags(run, n, "run"), _pointers(sum_out, n),
+                                           _pointers(out, n), _pointers(out_scale, n), _stream())
+    _check(st, "sg_tile_gated_norm")
+    return out
+
+
+def make_int8_linear_problem(rows, channels, outputs, dtype, activation=None):
+    """sg_int8_linear_problem of packed rows; other strides: set the fields.  activation: None or "gelu" (the tanh form)."""
+    return sg_int8_linear_problem(rows=int(rows), channels=int(channels), outputs=int(outputs), dtype=_DTYPES[dtype],
+                                  activation=_ACTIVATIONS[activation], x_stride=int(channels), w_stride=int(channels), out_stride=int(outputs))
+
+
+def sg_int8_linear_validate(p):
+    return load_library().sg_int8_linear_validate(ctypes.byref(p))
+
+
+def sg_tile_int8_linear(p, x, x_scale, w, w_scale, out, bias=None, run=None):
+    """x (int8), x_scale (float32), out: lists of one tensor per tile; w: int8; w_scale: float32; bias: `outputs` elements or None; run: uint8 or bool."""
+    n, torch = len(x), _torch()
+    for t in x_scale:
+        _vector(t, (torch.float32,), p.rows, "x_scale")
+    for t in (w, *x):
+        if t.dtype != torch.int8:
+            raise TypeError("x and w must be torch.int8, not %s" % t.dtype)
+    st = load_library().sg_tile_int8_linear(ctypes.byref(p), n, _ptr_array(x), _pointers(x_scale, n), _ptr(w),
+                                            _vector(w_scale, (torch.float32,), p.outputs, "w_scale"), _ptr(bias), _flags(run, n, "run"),
+                                            _pointers(out, n), _stream())
+    _check(st, "sg_tile_int8_linear")
     return out

@@ -14,7 +14,7 @@ C_CLIENT = os.path.join(ROOT, "tests", "c_client", "gpu_client.bin")
 SOURCES = ["sg_api.hip", "attention_bf16.hip", "attention_bf16_short.hip", "attention_f32.hip", "attention_f32_split.hip", "blend.hip",
            "gate.hip", "gate_static.hip", "region.hip", "similarity.hip", "context_api.hip",
            "context_bf16_wide.hip", "context_bf16_split.hip", "context_bf16_resident.hip", "context_f32.hip", "context_join.hip",
-           "residual_norm.hip"]
+           "residual_norm.hip", "block_api.hip", "rotary.hip", "gated_norm.hip", "int8_linear.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # packed fp32 VALU forms are kept out of the generated code on the test machines
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

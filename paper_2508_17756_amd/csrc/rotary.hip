@@ -1,0 +1,249 @@
+// Rotary positions of the queries and keys of tiles (sg_tile_rotary): pair (a, b) -> (a cos w - b sin w, b cos w + a sin w), w = frequency * position,
+// with or without a root-mean-square norm of each head before it.
+//
+// A workgroup takes a few tokens of a tile with all their heads (or a part of them): it computes the tokens' sines and cosines once, into LDS, and then
+// passes over the heads, each lane with 16 channels of one head as two vectors of 8 whose pairs lie in the lane.  The angle is a product in fp64
+// (positions reach millions of turns), reduced to a part of one turn there, and only that is rounded to fp32.  Bound by memory: every
+// channel is read and written once.
+#include "block_api.h"
+#include "row_common.h"
+
+namespace sg {
+namespace {
+
+constexpr int kRotaryTilesPerLaunch = 32;
+struct RotaryTable {
+  const void* q[kRotaryTilesPerLaunch];
+  const void* k[kRotaryTilesPerLaunch];
+  void* q_out[kRotaryTilesPerLaunch];
+  void* k_out[kRotaryTilesPerLaunch];
+  const int32_t* positions[kRotaryTilesPerLaunch];
+  int32_t origin[kRotaryTilesPerLaunch][3];
+};
+struct RotaryArgs {
+  const double* frequencies;
+  const void* q_weight;
+  const void* k_weight;
+  const uint8_t* run;
+  int64_t q_token, q_head, qo_token, qo_head, k_token, k_head, ko_token, ko_head;
+  int32_t tokens, chunk, chunk_shift, chunks;   // of a tile; tokens of a workgroup (2^chunk_shift); workgroups of a tile
+  int32_t heads, all_heads;                     // of q; of q and k
+  int32_t head_step;                            // heads of a workgroup: blockIdx.y takes head_step of them
+  int32_t channels, n_vec, lanes, lane_shift;   // of a head; vectors of 8; lanes of a head (a power of two)
+  int32_t turned, first_y, first_x;             // channels that turn; first pair of the axes y and x
+  int32_t H_W, W, position_axes;
+  int32_t canvas[3];
+  Divisor by_plane, by_row, by_chunks, by_heads;
+  bool by_token;                                // rows in the order of memory: heads of a token side by side
+  float eps;
+};
+
+template <typename T, bool HALF>
+__global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const RotaryTable tab) {
+  extern __shared__ float turns[];   // [chunk][pairs padded to 8] cosines, then sines
+  const int tile = (int)divide(blockIdx.x, a.by_chunks);
+  if (a.run && a.run[tile] == 0) return;
+  const int token0 = (int)(blockIdx.x - (uint32_t)tile * (uint32_t)a.chunks) << a.chunk_shift;
+  const int n_tokens = a.tokens - token0 < a.chunk ? a.tokens - token0 : a.chunk;
+  const int pairs = a.turned >> 1, row_pairs = (pairs + 7) & ~7;
+  float* const cosines = turns;
+  float* const sines = turns + a.chunk * row_pairs;
+
+  for (int i = threadIdx.x; i < n_tokens * row_pairs; i += 256) {
+    const int t = i / row_pairs, pair = i - t * row_pairs;
+    if (pair >= pairs) continue;
+    const int token = token0 + t;
+    const int axis = (pair >= a.first_y) + (pair >= a.first_x);
+    int position;
+    if (tab.positions[tile]) {
+      position = a.position_axes == 1 ? tab.positions[tile][token] : tab.positions[tile][3 * (int64_t)token + axis];
+    } else {
+      const int frame = (int)divide((uint32_t)token, a.by_plane), rest = token - frame * a.H_W;
+      const int y = (int)divide((uint32_t)rest, a.by_row);
+      position = tab.origin[tile][axis] + (axis == 0 ? frame : axis == 1 ? y : rest - y * a.W);
+      if (a.canvas[axis] > 0) position = (int)((uint32_t)position % (uint32_t)a.canvas[axis]);   // (the origin lies inside the canvas)
+    }
+    double turn = (double)position * (a.frequencies[pair] * 0.15915494309189535);   // 1 / (2 pi)
+    turn -= __builtin_rint(turn);
+    float sine, cosine;
+    sincospif(2.f * (float)turn, &sine, &cosine);
+    cosines[i] = cosine;
+    sines[i] = sine;
+  }
+  __syncthreads();
+
+  const int head0 = blockIdx.y * a.head_step;
+  const int n_heads = a.all_heads - head0 < a.head_step ? a.all_heads - head0 : a.head_step;
+  const int n_rows = n_heads * n_tokens;
+  const int l = threadIdx.x & (a.lanes - 1);
+  // The lane's vectors: HALF: those of the channels that turn meet their partners, half of them behind; the others two by two.
+  const int half = a.turned >> 4;
+  const bool has_a = 2 * l < a.n_vec || (!HALF && l < (a.n_vec + 1) / 2);
+  int va, vb;
+  if (HALF) {
+    va = l < half ? l : 2 * l;
+    vb = l < half ? l + half : 2 * l + 1;
+  } else {
+    va = l;
+    vb = l + (a.n_vec + 1) / 2;
+  }
+  const bool has_b = has_a && vb < a.n_vec;
+  for (int r = threadIdx.x >> a.lane_shift; r < n_rows; r += 256 >> a.lane_shift) {
+    int t, head;
+    if (a.by_token) {
+      t = n_heads == a.all_heads ? (int)divide((uint32_t)r, a.by_heads) : r / n_heads;
+      head = r - t * n_heads;
+    } else {
+      head = n_tokens == a.chunk ? r >> a.chunk_shift : r / n_tokens;
+      t = r - head * n_tokens;
+    }
+    head += head0;
+    const bool is_k = head >= a.heads;
+    const int64_t token = token0 + t;
+    const T* x;
+    T* y;
+    const T* weight;
+    if (is_k) {
+      const int h = head - a.heads;
+      x = (const T*)tab.k[tile] + token * a.k_token + h * a.k_head;
+      y = (T*)tab.k_out[tile] + token * a.ko_token + h * a.ko_head;
+      weight = (const T*)a.k_weight;
+    } else {
+      x = (const T*)tab.q[tile] + token * a.q_token + head * a.q_head;
+      y = (T*)tab.q_out[tile] + token * a.qo_token + head * a.qo_head;
+      weight = (const T*)a.q_weight;
+    }
+    Chan8<T> ra, rb;
+    if (has_a) ra.stream(x + 8 * va);
+    if (has_b) rb.stream(x + 8 * vb);
+    float u[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      u[e] = has_a ? ra.get(e) : 0.f;
+      v[e] = has_b ? rb.get(e) : 0.f;
+    }
+    if (a.q_weight || a.k_weight) {   // (the lanes of a row agree on `weight`)
+      float sq = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sq += u[e] * u[e] + v[e] * v[e];
+      const float mean = sum_over_lanes(sq, a.lanes) / (float)a.channels + a.eps;
+      float norm = rsqrtf(mean), by = 1.f;
+      const bool odd = !(mean >= kLeastMean && mean <= kMostFloat);
+      if (__any(odd)) {
+        const float to = mean < kLeastMean ? kGrowRow : kShrinkRow;
+        sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq += (u[e] * to) * (u[e] * to) + (v[e] * to) * (v[e] * to);
+        const float other = rsqrtf(sum_over_lanes(sq, a.lanes) / (float)a.channels + a.eps * to * to);
+        if (odd) { norm = other; by = to; }
+      }
+      if (weight) {
+        Chan8<T> wa, wb;
+        if (has_a) wa.load(weight + 8 * va);
+        if (has_b) wb.load(weight + 8 * vb);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (has_a) u[e] = u[e] * by * norm * wa.get(e);
+          if (has_b) v[e] = v[e] * by * norm * wb.get(e);
+        }
+      }
+    }
+    const float* const c = cosines + t * row_pairs;
+    const float* const s = sines + t * row_pairs;
+    if (HALF) {
+      if (l < half) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float cs = c[8 * l + e], sn = s[8 * l + e], p = u[e], q = v[e];
+          u[e] = p * cs - q * sn;
+          v[e] = q * cs + p * sn;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (4 * va + e < pairs) {
+          const float cs = c[4 * va + e], sn = s[4 * va + e], p = u[2 * e], q = u[2 * e + 1];
+          u[2 * e] = p * cs - q * sn;
+          u[2 * e + 1] = q * cs + p * sn;
+        }
+        if (4 * vb + e < pairs) {
+          const float cs = c[4 * vb + e], sn = s[4 * vb + e], p = v[2 * e], q = v[2 * e + 1];
+          v[2 * e] = p * cs - q * sn;
+          v[2 * e + 1] = q * cs + p * sn;
+        }
+      }
+    }
+    if (has_a) stream8(y + 8 * va, u);
+    if (has_b) stream8(y + 8 * vb, v);
+  }
+}
+
+}  // namespace
+
+int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q, const void* const* k, const double* frequencies,
+                  const int32_t* origin, const int32_t* const* positions, const void* q_weight, const void* k_weight, const uint8_t* run,
+                  void* const* q_out, void* const* k_out, hipStream_t s) {
+  RotaryArgs a = {};
+  a.frequencies = frequencies; a.q_weight = q_weight; a.k_weight = k ? k_weight : nullptr;
+  a.q_token = p.q_stride_token; a.q_head = p.q_stride_head; a.qo_token = p.q_out_stride_token; a.qo_head = p.q_out_stride_head;
+  a.k_token = p.k_stride_token; a.k_head = p.k_stride_head; a.ko_token = p.k_out_stride_token; a.ko_head = p.k_out_stride_head;
+  a.tokens = p.T * p.H * p.W;
+  a.heads = p.heads; a.all_heads = p.heads + (k ? p.kv_heads : 0);
+  a.channels = p.head_dim; a.n_vec = p.head_dim / 8;
+  a.lanes = 1; a.lane_shift = 0;
+  while (2 * a.lanes < a.n_vec) { a.lanes <<= 1; ++a.lane_shift; }
+  a.turned = p.axis_t + p.axis_y + p.axis_x;
+  a.first_y = p.axis_t / 2; a.first_x = (p.axis_t + p.axis_y) / 2;
+  a.H_W = p.H * p.W; a.W = p.W; a.position_axes = p.position_axes;
+  a.canvas[0] = p.canvas_t; a.canvas[1] = p.canvas_h; a.canvas[2] = p.canvas_w;
+  a.by_plane = make_divisor((uint32_t)a.H_W); a.by_row = make_divisor((uint32_t)p.W);
+  a.by_heads = make_divisor((uint32_t)a.all_heads);
+  a.by_token = p.q_stride_head < p.q_stride_token;
+  a.eps = p.eps;
+  // Tokens of a workgroup: enough rows for 8 passes of it, its table within 32 KiB.
+  const int rows_per_pass = 256 >> a.lane_shift, row_pairs = (a.turned / 2 + 7) & ~7;
+  a.chunk = 1; a.chunk_shift = 0;
+  while (a.chunk < 64 && a.chunk < a.tokens && (int64_t)a.chunk * a.all_heads < 8 * rows_per_pass && 2 * a.chunk * row_pairs * 8 <= 32768) {
+    a.chunk <<= 1; ++a.chunk_shift;
+  }
+  a.chunks = (a.tokens + a.chunk - 1) / a.chunk;
+  a.by_chunks = make_divisor((uint32_t)a.chunks);
+  const size_t lds = (size_t)a.chunk * row_pairs * 8;
+  for (int t0 = 0; t0 < n_tiles; t0 += kRotaryTilesPerLaunch) {
+    const int n = n_tiles - t0 < kRotaryTilesPerLaunch ? n_tiles - t0 : kRotaryTilesPerLaunch;
+    RotaryTable tab = {};
+    for (int i = 0; i < n; ++i) {
+      tab.q[i] = q[t0 + i];
+      tab.q_out[i] = q_out[t0 + i];
+      tab.k[i] = k ? k[t0 + i] : nullptr;
+      tab.k_out[i] = k ? k_out[t0 + i] : nullptr;
+      tab.positions[i] = positions ? positions[t0 + i] : nullptr;
+      for (int j = 0; j < 3 && origin; ++j) {
+        int64_t at = origin[3 * (t0 + i) + j];
+        if (a.canvas[j] > 0) at = (at % a.canvas[j] + a.canvas[j]) % a.canvas[j];
+        tab.origin[i][j] = (int32_t)at;
+      }
+    }
+    a.run = run ? run + t0 : nullptr;
+    // Few tokens: their heads go to several workgroups, one pass each.
+    int splits = 1;
+    const int64_t wgs = (int64_t)n * a.chunks;
+    const int passes = (int)(((int64_t)a.chunk * a.all_heads + rows_per_pass - 1) / rows_per_pass);
+    while (splits < passes && wgs * splits < 512) ++splits;
+    a.head_step = (a.all_heads + splits - 1) / splits;
+    splits = (a.all_heads + a.head_step - 1) / a.head_step;
+    const dim3 grid((unsigned)wgs, (unsigned)splits);
+    if (p.dtype == SG_F32) {
+      if (p.layout == SG_ROTARY_HALF) rotary_kernel<float, true><<<grid, 256, lds, s>>>(a, tab);
+      else rotary_kernel<float, false><<<grid, 256, lds, s>>>(a, tab);
+    } else {
+      if (p.layout == SG_ROTARY_HALF) rotary_kernel<uint16_t, true><<<grid, 256, lds, s>>>(a, tab);
+      else rotary_kernel<uint16_t, false><<<grid, 256, lds, s>>>(a, tab);
+    }
+    SG_HIP_TRY(hipGetLastError());
+  }
+  return SG_OK;
+}
+
+}  // namespace sg
