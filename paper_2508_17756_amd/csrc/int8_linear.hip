@@ -1,10 +1,15 @@
 // Linear layer of tiles in 8-bit integers (sg_tile_int8_linear):
 //     out[r][o] = act(x_scale[r] * w_scale[o] * sum_c x[r][c] w[o][c] + bias[o])
 // Rows of all tiles of a launch that run are numbered one behind the other; a workgroup computes BM of them times BN outputs.  Both operands have their
-// channels side by side in memory, as the matrix instruction wants them (32x32x32: a lane gives 16 channels of one row), so 128 channels of the
-// block's rows of x and w go straight into LDS, 16 bytes a lane, one stage ahead of the products.  The 16-byte pieces of a row
-// are stored in the order piece ^ (row mod 8): 8 lanes that read the same piece of 8 rows then meet 8 different groups of banks.
-// w is the instruction's first operand: a lane then holds 4 outputs side by side of one row, which it scales and stores together.
+// channels side by side in memory, as the matrix instruction wants them (16x16x64: a lane gives 16 channels of one row), so 128 channels of the
+// block's rows of x and w go straight into LDS, 16 bytes a lane, a stage or more ahead of the products.  The 16-byte pieces of a row
+// are stored in the order piece ^ (row / 2 mod 8): 16 lanes that read the same piece of 16 rows then meet 16 different groups of the 64 banks.
+// w is the instruction's first operand, its rows in an order that leaves a lane with outputs side by side of one row, which it scales and stores together.
+//
+// Large calls are bound by the power that the products take: held in registers, N(0, 32)-distributed integers pass the instruction at 3.9 POP/s (zeros: 4.9;
+// the form 32x32x32, which touches each sum twice as often, at 3.3).  Blocks of 256 x 256: 34,560 x 5,120 x 15,360 2.35 ms = 2.31 POP/s (with 32x32x32: 2.58),
+// 75,600 x 5,120 x 20,480 with GELU 7.1 - 7.4 ms = 2.14 - 2.22 POP/s; on zeros the former takes 2.07.
+#include <atomic>
 #include "block_api.h"
 #include "row_common.h"
 
@@ -12,9 +17,8 @@ namespace sg {
 namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kLinearTilesPerLaunch = 64;
+constexpr int kLinearTilesPerLaunch = 64, kMaxDevices = 64;
 struct LinearTable {
   const void* x[kLinearTilesPerLaunch];
   const float* x_scale[kLinearTilesPerLaunch];
@@ -32,27 +36,36 @@ struct LinearArgs {
   bool gelu;
 };
 
-// What lanes read of places behind the channels' end.
-__device__ const u32x4 kNoChannels = {0, 0, 0, 0};
-
-constexpr int kStageBytes = 128;   // channels of a stage
+// What lanes read of places behind the channels' end: 16 bytes at a time, up to STAGES + 1 stages behind one another.
+__device__ __align__(16) const char kNoChannels[2048] = {};
 
 __device__ __forceinline__ float gelu(float v) {   // v (1 + tanh(u)) / 2 = v / (1 + exp(-2 u)),  u = sqrt(2 / pi) (v + 0.044715 v^3)
   const float u = v * (-2.3022081983f - 0.1029432402f * v * v);   // -2 u log2(e)
-  return v / (1.f + exp2f(u));
+  return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u));
 }
 
-__device__ __forceinline__ void store4(uint16_t* p, const float (&v)[4]) { *(u32x2*)p = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])}; }
-__device__ __forceinline__ void store4(float* p, const float (&v)[4]) { *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]}; }
-__device__ __forceinline__ void load4(const uint16_t* p, float (&v)[4]) {
-  const u32x2 w = *(const u32x2*)p;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = e & 1 ? __uint_as_float(w[e >> 1] & 0xffff0000u) : __uint_as_float(w[e >> 1] << 16);
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+  *(u32x4*)p = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
 }
-__device__ __forceinline__ void load4(const float* p, float (&v)[4]) {
-  const f32x4 w = *(const f32x4*)p;
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+  *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+
+// 8 outputs side by side of a row, from output o on.
+template <typename T> __device__ __forceinline__ void finish8(const LinearArgs& a, const int (&sum)[8], float x_scale, int o, T* out) {
+  Chan8<float> ws;
+  ws.load(a.w_scale + o);
+  Chan8<T> b;
+  if (a.bias) b.load((const T*)a.bias + o);
+  float v[8];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = w[e];
+  for (int e = 0; e < 8; ++e) {
+    v[e] = (float)sum[e] * x_scale;
+    v[e] = a.bias ? fmaf(v[e], ws.get(e), b.get(e)) : v[e] * ws.get(e);
+    if (a.gelu) v[e] = gelu(v[e]);
+  }
+  store8(out, v);
 }
 
 // The tiles of a launch that run, in their order; false if there are none.  list: LDS.  (All threads of the workgroup.)
@@ -75,12 +88,14 @@ __device__ __forceinline__ void block_of(uint32_t id, uint32_t gm, uint32_t gn, 
   m = group * 8 + rest - n * tall;
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearArgs a, const LinearTable tab) {
-  constexpr int kWaves = WM * WN, kRows = BM + BN, kLoads = kRows / 8 / kWaves;
-  constexpr int FM = BM / WM / 32, FN = BN / WN / 32;   // 32 x 32 results of a wavefront
-  static_assert(kRows % (8 * kWaves) == 0 && FM * WM * 32 == BM && FN * WN * 32 == BN, "tiles");
-  extern __shared__ __align__(1024) char lds[];   // [2 stages][BM rows of x, BN rows of w][128]
+  constexpr int BK = 128;   // channels of a stage
+  constexpr int kWaves = WM * WN, kRows = BM + BN, kLoads = kRows / 8 / kWaves, kStageBytes = kRows * BK, kAhead = (STAGES - 2) * kLoads;
+  constexpr int FM = BM / WM / 16, FN = BN / WN / 16;   // 16 x 16 results of a wavefront
+  static_assert(kRows % (8 * kWaves) == 0 && kWaves % 2 == 0 && FM * WM * 16 == BM && FN * WN * 16 == BN && FM % 2 == 0 && FN % 2 == 0, "tiles");
+  static_assert((STAGES + 1) * BK + 16 <= (int)sizeof(kNoChannels) && kAhead + kLoads < 64, "loads behind the end, loads in flight");
+  extern __shared__ __align__(1024) char lds[];   // [STAGES][BM rows of x, BN rows of w][BK]
   __shared__ int list[kLinearTilesPerLaunch];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t total = (uint32_t)running_tiles(a, list) * (uint32_t)a.rows;
@@ -96,9 +111,9 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
     return (int64_t)(r - i * (uint32_t)a.rows);
   };
 
-  // One 1 KiB piece of a stage, 8 rows, is a load of a wavefront: lane i fills place i mod 8 of row i / 8.
+  // One 1 KiB piece of a stage, 8 rows, is a load of a wavefront: lane i fills the i-th 16 bytes.
   const char* from[kLoads];
-  const int channel = 16 * ((lane & 7) ^ (lane >> 3));
+  const int channel = 16 * ((lane & 7) ^ ((wave & 1) << 2 | lane >> 4));
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
     const int row = (wave + j * kWaves) * 8 + (lane >> 3);
@@ -107,85 +122,284 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
       const int64_t at = row_at(m0 + row, tile);
       from[j] = (const char*)tab.x[tile] + at * a.x_stride + channel;
     } else {
-      const int o = n0 + row - BM;
+      // Row 16 i + r of a wavefront's outputs is output 4 FN (r / 4) + 4 i + r mod 4 of them: what a lane gets is then side by side.
+      const int w = (row - BM) % (16 * FN), r = w & 15;
+      const int o = n0 + row - BM - w + 4 * FN * (r >> 2) + 4 * (w >> 4) + (r & 3);
       from[j] = a.w + (int64_t)(o < a.outputs ? o : a.outputs - 1) * a.w_stride + channel;
     }
   }
-  const uint32_t lds_at = (uint32_t)(uintptr_t)(SG_LDS char*)lds;
-  auto load = [&](int stage, int buffer) {
-    const bool there = stage * kStageBytes + channel < a.channels;
+  const int stages = (a.channels + BK - 1) / BK;
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(SG_LDS char*)lds + wave * 1024;
+  auto load = [&](int j, int buffer) {
+    dma16_addr(from[j], __builtin_amdgcn_readfirstlane(lds_at + buffer * kStageBytes + j * kWaves * 1024));
+    from[j] += BK;
+  };
+  // The last stage may have fewer channels, and as many loads follow it as are in flight: zeros.
+  auto check_end = [&](int stage) {
+    if (stage == stages - 1 ? stage * BK + channel >= a.channels : stage == stages) {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const char* const p = there ? from[j] + (int64_t)stage * kStageBytes : (const char*)&kNoChannels;
-      dma16_addr(p, __builtin_amdgcn_readfirstlane(lds_at + buffer * (kRows * kStageBytes) + (wave + j * kWaves) * 1024));
+      for (int j = 0; j < kLoads; ++j) from[j] = kNoChannels;
     }
   };
 
-  i32x16 acc[FN][FM] = {};
+  // A stage is two steps of 64 channels, a step FM groups of products with 16 rows each.  xf: the rows, read for the next step as soon as their
+  // group is out; wf: the outputs, of this step and the next.
+  i32x4 acc[FN][FM] = {}, xf[FM], wf[2][FN];
   const int wm = wave % WM, wn = wave / WM;
-  const int r32 = lane & 31;
-  const int stages = (a.channels + kStageBytes - 1) / kStageBytes;
-  load(0, 0);
-  for (int k = 0; k < stages; ++k) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (k + 1 < stages) load(k + 1, (k + 1) & 1);
-    const char* const xs = lds + (k & 1) * (kRows * kStageBytes) + (wm * FM * 32 + r32) * kStageBytes;
-    const char* const ws = lds + (k & 1) * (kRows * kStageBytes) + (BM + wn * FN * 32 + r32) * kStageBytes;
+  const int r16 = lane & 15, quarter = lane >> 4;
+  auto at = [&](int buffer, int c, int row) {   // what the lane gives of 16 rows at step c
+    return (const i32x4*)(lds + buffer * kStageBytes + (row + r16) * BK + 16 * ((4 * c + quarter) ^ (r16 >> 1)));
+  };
+  auto read_x = [&](int buffer, int c, int j) { xf[j] = *at(buffer, c, (wm * FM + j) * 16); };
+  auto read_w = [&](int buffer, int c, int i) { wf[c][i] = *at(buffer, c, BM + (wn * FN + i) * 16); };
+  // Group j of step c; what `between` reads or loads goes out in the shadow of its products.
+  auto group = [&](int c, int j, auto between) {
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int c = 0; c < kStageBytes / 32; ++c) {
-      const int place = 16 * ((2 * c + (lane >> 5)) ^ (lane & 7));
-      i32x4 xf[FM], wf[FN];
-#pragma unroll
-      for (int i = 0; i < FM; ++i) xf[i] = *(const i32x4*)(xs + i * 32 * kStageBytes + place);
-#pragma unroll
-      for (int i = 0; i < FN; ++i) wf[i] = *(const i32x4*)(ws + i * 32 * kStageBytes + place);
-#pragma unroll
-      for (int i = 0; i < FN; ++i)
-#pragma unroll
-        for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[i], xf[j], acc[i][j], 0, 0, 0);
+    for (int i = 0; i < FN; ++i) {
+      acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[c][i], xf[j], acc[i][j], 0, 0, 0);
+      if (i == FN / 2 - 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        between();
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  constexpr int kReads = (FN + FM - 1) / FM;
+  auto first_step = [&](int buffer) {
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+      group(0, j, [&] {
+#pragma unroll
+        for (int i = j * kReads; i < (j + 1) * kReads; ++i)
+          if (i < FN) read_w(buffer, 1, i);
+      });
+      read_x(buffer, 1, j);
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < STAGES; ++k) {
+    check_end(k);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load(j, k);
   }
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"(kAhead + kLoads) : "memory");
+#pragma unroll
+  for (int i = 0; i < FN; ++i) read_w(0, 0, i);
+#pragma unroll
+  for (int j = 0; j < FM; ++j) read_x(0, 0, j);
+  first_step(0);
+#pragma unroll
+  for (int j = 0; j < FM / 2; ++j) group(1, j, [] {});
+  // The barrier stands in the middle of the second step: by then every read of the stage has long been issued, and the other half of the products covers
+  // the first reads of the next stage.
+  int buffer = 0;
+  for (int k = 0; k + 1 < stages; ++k) {
+    const int next = buffer + 1 == STAGES ? 0 : buffer + 1;
+    check_end(k + STAGES);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(kAhead) : "memory");
+    constexpr int kHalf = FM / 2, kLoadsPer = (kLoads + kHalf - 1) / kHalf, kWPer = (FN + kHalf - 1) / kHalf;
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) {
+      group(1, kHalf + j, [&] {
+#pragma unroll
+        for (int i = j * kWPer; i < (j + 1) * kWPer; ++i)
+          if (i < FN) read_w(next, 0, i);
+        read_x(next, 0, j);
+#pragma unroll
+        for (int l = j * kLoadsPer; l < (j + 1) * kLoadsPer; ++l)
+          if (l < kLoads) load(l, buffer);
+      });
+      read_x(next, 0, kHalf + j);
+    }
+    buffer = next;
+    first_step(buffer);
+#pragma unroll
+    for (int j = 0; j < kHalf; ++j) group(1, j, [] {});
+  }
+#pragma unroll
+  for (int j = FM / 2; j < FM; ++j) group(1, j, [] {});
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing arrives in LDS that is another workgroup's by then
 
-  // Lane: row r32 of each 32 rows; outputs 8 g + 4 (lane / 32) + 0 .. 3 in registers 4 g + 0 .. 3.
+  // Lane: row r16 of each 16 rows; 4 FN outputs side by side.
+  const int o0 = n0 + (wn * 4 + quarter) * 4 * FN;
+  if (o0 >= a.outputs) return;
 #pragma unroll
   for (int j = 0; j < FM; ++j) {
-    const uint32_t r = m0 + (wm * FM + j) * 32 + r32;
+    const uint32_t r = m0 + (wm * FM + j) * 16 + r16;
     if (r >= total) continue;
     int tile;
     const int64_t row = row_at(r, tile);
     const float xs = tab.x_scale[tile][row];
     T* const out = (T*)tab.out[tile] + row * a.o_stride;
 #pragma unroll
-    for (int i = 0; i < FN; ++i)
+    for (int i = 0; i < FN; i += 2) {
+      const int o = o0 + 4 * i;
+      if (o >= a.outputs) continue;
+      int v[8];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int o = n0 + (wn * FN + i) * 32 + 8 * g + 4 * (lane >> 5);
-        if (o >= a.outputs) continue;
-        const f32x4 ws = *(const f32x4*)(a.w_scale + o);
-        float b[4] = {0.f, 0.f, 0.f, 0.f}, v[4];
-        if (a.bias) load4((const T*)a.bias + o, b);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] = fmaf((float)acc[i][j][4 * g + e] * xs, ws[e], b[e]);
-          if (a.gelu) v[e] = gelu(v[e]);
-        }
-        store4(out + o, v);
-      }
+      for (int e = 0; e < 8; ++e) v[e] = acc[i + e / 4][j][e % 4];
+      finish8<T>(a, v, xs, o, out + o);
+    }
   }
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+// Few rows: the weights' bytes are what counts.  A workgroup takes 16 MT rows and 16 NT outputs; its wavefronts take the channels in turn, 128 at a time, each
+// through a ring of DEPTH stages in LDS that is its own, so that no wavefront waits for another before the end.  Their sums meet in LDS: integers, so the
+// order does not matter.
+template <typename T, int MT, int NT, int DEPTH, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void int8_linear_rows_kernel(const LinearArgs a, const LinearTable tab) {
+  constexpr int BK = 128, kRows = 16 * (MT + NT), kLoads = kRows / 8, kStageBytes = kRows * BK, kPitch = 16 * NT + 4, kThreads = 64 * WAVES;
+  static_assert((DEPTH - 1) * kLoads < 64, "loads in flight");
+  extern __shared__ __align__(1024) char lds[];   // [WAVES][DEPTH][rows of x, rows of w][128]
+  __shared__ int list[kLinearTilesPerLaunch];
+  __shared__ int sums[16 * MT * kPitch];          // [row][output]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t total = (uint32_t)running_tiles(a, list) * (uint32_t)a.rows;
+  const uint32_t m0 = blockIdx.y * 16 * MT;
+  const int n0 = blockIdx.x * 16 * NT;
+  if (m0 >= total) return;
+  const int stages = (a.channels + BK - 1) / BK, n = (stages - wave + WAVES - 1) / WAVES;   // of the wavefront: stage k WAVES + wave
+  const char* from[kLoads];
+  int channel[2];   // of the pieces with even and odd numbers
+#pragma unroll
+  for (int j = 0; j < 2; ++j) channel[j] = 16 * ((lane & 7) ^ (j << 2 | lane >> 4));
+#pragma unroll
+  for (int j = 0; j < kLoads; ++j) {
+    const int row = 8 * j + (lane >> 3);
+    if (row < 16 * MT) {
+      uint32_t r = m0 + row;
+      r = r < total ? r : total - 1;
+      const uint32_t i = divide(r, a.by_rows);
+      from[j] = (const char*)tab.x[list[i]] + (int64_t)(r - i * (uint32_t)a.rows) * a.x_stride;
+    } else {
+      const int o = n0 + row - 16 * MT;
+      from[j] = a.w + (int64_t)(o < a.outputs ? o : a.outputs - 1) * a.w_stride;
+    }
+    from[j] += wave * BK + channel[j & 1];
+  }
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(SG_LDS char*)lds + wave * (DEPTH * kStageBytes);
+  auto load = [&](int k, int slot) {
+    const bool last = k * WAVES + wave == stages - 1;   // zeros behind the channels' end
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const char* const p = last && (stages - 1) * BK + channel[j & 1] >= a.channels ? kNoChannels : from[j];
+      dma16_addr(p, __builtin_amdgcn_readfirstlane(lds_at + slot * kStageBytes + j * 1024));
+      from[j] += WAVES * BK;
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < DEPTH; ++k)
+    if (k < n) load(k, k);
+  for (int i = threadIdx.x; i < 16 * MT * kPitch; i += kThreads) sums[i] = 0;
+  const int r16 = lane & 15, quarter = lane >> 4;
+  i32x4 acc[NT][MT] = {};
+  const char* const mine = lds + wave * (DEPTH * kStageBytes) + r16 * BK;
+  int slot = 0;
+  for (int k = 0; k < n; ++k) {
+    if (k + DEPTH <= n) asm volatile("s_waitcnt vmcnt(%0)" : : "n"((DEPTH - 1) * kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    i32x4 xf[2][MT], wf[2][NT];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const char* const at = mine + slot * kStageBytes + 16 * ((4 * c + quarter) ^ (r16 >> 1));
+#pragma unroll
+      for (int i = 0; i < NT; ++i) wf[c][i] = *(const i32x4*)(at + (MT + i) * 16 * BK);
+#pragma unroll
+      for (int j = 0; j < MT; ++j) xf[c][j] = *(const i32x4*)(at + j * 16 * BK);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (k + DEPTH < n) load(k + DEPTH, slot);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[c][i], xf[c][j], acc[i][j], 0, 0, 0);
+    slot = slot + 1 == DEPTH ? 0 : slot + 1;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) atomicAdd(&sums[(16 * j + r16) * kPitch + 16 * i + 4 * quarter + e], acc[i][j][e]);
+  __syncthreads();
+  for (int t = threadIdx.x; t < 16 * MT * 2 * NT; t += kThreads) {
+    const int row_in = t / (2 * NT), o = n0 + 8 * (t - row_in * 2 * NT);
+    const uint32_t r = m0 + row_in;
+    if (r >= total || o >= a.outputs) continue;
+    const uint32_t i = divide(r, a.by_rows);
+    const int tile = list[i];
+    const int64_t row = r - i * (uint32_t)a.rows;
+    const int* const sum = sums + row_in * kPitch + (o - n0);
+    int v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = sum[e];
+    finish8<T>(a, v, tab.x_scale[tile][row], o, (T*)tab.out[tile] + row * a.o_stride + o);
+  }
+}
+
+// The kernel's dynamic-LDS limit, raised once on each device.
+inline int raise_lds(const void* kernel, size_t bytes, std::atomic<bool>* raised) {
+  int dev = -1;
+  if (bytes <= 49152) return SG_OK;
+  SG_HIP_TRY(hipGetDevice(&dev));
+  if (dev < 0 || dev >= kMaxDevices || !raised[dev].load(std::memory_order_acquire)) {
+    SG_HIP_TRY(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+    if (dev >= 0 && dev < kMaxDevices) raised[dev].store(true, std::memory_order_release);
+  }
+  return SG_OK;
+}
+
+template <typename T, int BM, int BN, int WM, int WN, int STAGES>
 int launch(LinearArgs& a, const LinearTable& tab, hipStream_t s) {
   const uint64_t rows = (uint64_t)a.n_tiles * (uint64_t)a.rows;
   a.blocks_m = (uint32_t)((rows + BM - 1) / BM);
   a.blocks_n = (uint32_t)((a.outputs + BN - 1) / BN);
-  constexpr size_t kLds = 2 * (BM + BN) * kStageBytes;
-  auto* const kernel = int8_linear_kernel<T, BM, BN, WM, WN>;
-  if (kLds > 65536) SG_HIP_TRY(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds));
+  constexpr size_t kLds = STAGES * (BM + BN) * 128;
+  static std::atomic<bool> raised[kMaxDevices];
+  auto* const kernel = int8_linear_kernel<T, BM, BN, WM, WN, STAGES>;
+  const int st = raise_lds((const void*)kernel, kLds, raised);
+  if (st != SG_OK) return st;
   kernel<<<dim3(a.blocks_m * a.blocks_n), 64 * WM * WN, kLds, s>>>(a, tab);
   SG_HIP_TRY(hipGetLastError());
   return SG_OK;
+}
+
+template <typename T, int MT, int NT, int DEPTH, int WAVES> int launch_rows(const LinearArgs& a, const LinearTable& tab, hipStream_t s) {
+  const int64_t rows = (int64_t)a.n_tiles * a.rows;
+  const dim3 grid((unsigned)((a.outputs + 16 * NT - 1) / (16 * NT)), (unsigned)((rows + 16 * MT - 1) / (16 * MT)));
+  constexpr size_t kLds = WAVES * DEPTH * 16 * (MT + NT) * 128;
+  static std::atomic<bool> raised[kMaxDevices];
+  auto* const kernel = int8_linear_rows_kernel<T, MT, NT, DEPTH, WAVES>;
+  const int st = raise_lds((const void*)kernel, kLds, raised);
+  if (st != SG_OK) return st;
+  kernel<<<grid, 64 * WAVES, kLds, s>>>(a, tab);
+  SG_HIP_TRY(hipGetLastError());
+  return SG_OK;
+}
+
+// Which blocks: those whose rounds over the compute units take least.  us for 40 stages of 128 channels and so many blocks, on 256 compute units:
+//   256 x 256   68 for each round of 256                                      (256 blocks 68, 480 145)
+//   128 x 128   42 for up to 256, then 46 for each round of 512               (240: 42, 480: 50, 960: 91, 1,920: 175)
+//    64 x 64    19 for up to 256, then 10 and 0.036 a block                   (320: 28, 960: 47, 2,560: 104)
+//    32 x 32, wavefronts apart   8 and 0.015 a block                          (160: 10.7, 640: 18, 1,280: 27, 2,560: 45)
+// and up to 16 rows: 16 x 32 with 8 wavefronts (5,120 channels and outputs, weights from memory: 8.2 - 9.4; 16 x 16 with 4 8.8 - 10.4, 32 x 32 8.7 - 9.6), or
+// 16 x 16 where that leaves most compute units without work (20,480 channels, 512 outputs: 15.4 instead of 22).
+template <typename T> int launch_best(LinearArgs& a, const LinearTable& tab, hipStream_t s) {
+  const int64_t rows = (int64_t)a.n_tiles * a.rows, outputs = a.outputs;
+  auto blocks = [&](int64_t bm, int64_t bn) { return ((rows + bm - 1) / bm) * ((outputs + bn - 1) / bn); };
+  if (rows <= 16) return blocks(16, 32) >= 64 ? launch_rows<T, 1, 2, 3, 8>(a, tab, s) : launch_rows<T, 1, 1, 4, 4>(a, tab, s);
+  const int64_t b256 = blocks(256, 256), b128 = blocks(128, 128), b64 = blocks(64, 64), b32 = blocks(32, 32);
+  const int64_t t256 = (b256 + 255) / 256 * 68000, t128 = b128 <= 256 ? 42000 : (b128 + 511) / 512 * 46000, t64 = b64 <= 256 ? 19000 : 10000 + 36 * b64,
+                t32 = 8000 + 15 * b32;
+  if (t32 <= t64 && t32 <= t128 && t32 <= t256) return launch_rows<T, 2, 2, 2, 4>(a, tab, s);
+  if (t64 <= t128 && t64 <= t256) return launch<T, 64, 64, 2, 2, 3>(a, tab, s);
+  if (t128 <= t256) return launch<T, 128, 128, 2, 2, 2>(a, tab, s);
+  return launch<T, 256, 256, 2, 4, 2>(a, tab, s);
 }
 
 }  // namespace
@@ -208,7 +422,7 @@ int launch_int8_linear(const sg_int8_linear_problem& p, int n_tiles, const void*
     }
     a.n_tiles = n;
     a.run = run ? run + t0 : nullptr;
-    const int st = p.dtype == SG_F32 ? launch<float, 128, 128, 2, 2>(a, tab, s) : launch<uint16_t, 128, 128, 2, 2>(a, tab, s);
+    const int st = p.dtype == SG_F32 ? launch_best<float>(a, tab, s) : launch_best<uint16_t>(a, tab, s);
     if (st != SG_OK) return st;
   }
   return SG_OK;
