@@ -587,6 +587,18 @@ def _vector(t, kinds, n, name):
     return t.data_ptr()
 
 
+def _vectors(tensors, kind, n, elements, name):
+    """_pointers of device arrays of `elements` each, checked as _vector does."""
+    if len(tensors) != n:
+        raise ValueError("%d tensors for %d tiles" % (len(tensors), n))
+    at = []
+    for t in tensors:
+        if t.dtype is not kind or t.numel() < elements or not t.is_cuda or not t.is_contiguous():
+            _vector(t, (kind,), elements, name)
+        at.append(t.data_ptr())
+    return (ctypes.c_void_p * (n or 1))(*at)
+
+
 def _lengths(t, n, name):
     return None if t is None else _vector(t, (_torch().int32,), n, name)
 
@@ -679,11 +691,9 @@ def sg_tile_rotary(p, q, q_out, frequencies, k=None, k_out=None, origin=None, po
         if len(origin) != n:
             raise ValueError("%d origins for %d tiles" % (len(origin), n))
         at = (ctypes.c_int32 * (3 * n or 1))(*[int(v) for o in origin for v in (o[0], o[1], o[2])])
-    if positions is not None:
-        for t in positions:
-            _vector(t, (torch.int32,), p.T * p.H * p.W * p.position_axes, "positions")
+    listed = None if positions is None else _vectors(positions, torch.int32, n, p.T * p.H * p.W * p.position_axes, "positions")
     st = load_library().sg_tile_rotary(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _vector(frequencies, (torch.float64,), pairs, "frequencies"), at,
-                                       _pointers(positions, n), _ptr(q_weight), _ptr(k_weight), _flags(run, n, "run"), _pointers(q_out, n),
+                                       listed, _ptr(q_weight), _ptr(k_weight), _flags(run, n, "run"), _pointers(q_out, n),
                                        _pointers(k_out, n), _stream())
     _check(st, "sg_tile_rotary")
     return q_out if k is None else (q_out, k_out)
@@ -726,12 +736,11 @@ def sg_int8_linear_validate(p):
 def sg_tile_int8_linear(p, x, x_scale, w, w_scale, out, bias=None, run=None):
     """x (int8), x_scale (float32), out: lists of one tensor per tile; w: int8; w_scale: float32; bias: `outputs` elements or None; run: uint8 or bool."""
     n, torch = len(x), _torch()
-    for t in x_scale:
-        _vector(t, (torch.float32,), p.rows, "x_scale")
+    int8 = torch.int8
     for t in (w, *x):
-        if t.dtype != torch.int8:
+        if t.dtype is not int8:
             raise TypeError("x and w must be torch.int8, not %s" % t.dtype)
-    st = load_library().sg_tile_int8_linear(ctypes.byref(p), n, _ptr_array(x), _pointers(x_scale, n), _ptr(w),
+    st = load_library().sg_tile_int8_linear(ctypes.byref(p), n, _ptr_array(x), _vectors(x_scale, torch.float32, n, p.rows, "x_scale"), _ptr(w),
                                             _vector(w_scale, (torch.float32,), p.outputs, "w_scale"), _ptr(bias), _flags(run, n, "run"),
                                             _pointers(out, n), _stream())
     _check(st, "sg_tile_int8_linear")

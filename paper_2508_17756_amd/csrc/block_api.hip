@@ -14,18 +14,27 @@ static bool tiles_ok(const void* const* a, int n, uintptr_t mask = 15u) {
   return true;
 }
 
-// Buffers that are written: written[i] may be read[i], with its stride, and no two tiles write one buffer or write what another tile reads.
-static bool written_apart(int n, void* const* written, const void* const* read, bool same_strides) {
-  const void* at[SG_MAX_TILES];
-  std::copy(written, written + n, at);
-  std::sort(at, at + n);
-  for (int i = 1; i < n; ++i)
-    if (at[i] == at[i - 1]) return false;
-  if (!read) return true;
-  for (int i = 0; i < n; ++i)
-    if (std::binary_search(at, at + n, read[i]) && !(same_strides && written[i] == read[i])) return false;
-  return true;
-}
+// Buffers that a call writes: no two tiles write one, and none is what another tile reads or what the call reads in another place.
+class Written {
+ public:
+  Written(void* const* written, int n) : written_(written), n_(n) {
+    std::copy(written, written + n, at_);
+    if (!std::is_sorted(at_, at_ + n)) std::sort(at_, at_ + n);
+  }
+  bool different() const { return std::adjacent_find(at_, at_ + n_) == at_ + n_; }
+  // read[i] may be written[i] where both have the same strides: in place.
+  bool apart_from(const void* const* read, bool same_strides = false) const {
+    if (!read) return true;
+    for (int i = 0; i < n_; ++i)
+      if (read[i] >= at_[0] && read[i] <= at_[n_ - 1] && std::binary_search(at_, at_ + n_, read[i]) && !(same_strides && written_[i] == read[i])) return false;
+    return true;
+  }
+
+ private:
+  void* const* written_;
+  int n_;
+  const void* at_[SG_MAX_TILES];
+};
 
 static bool row_stride_ok(int64_t stride, int64_t channels, int64_t unit) { return stride >= channels && !(stride % unit) && stride < (1ll << 40); }
 
@@ -131,12 +140,12 @@ int sg_tile_rotary(const sg_rotary_problem* p, int32_t n_tiles, const void* cons
       if (canvas[i % 3] == 0 && (int64_t)origin[i] + size[i % 3] - 1 > INT32_MAX) return SG_ERR_INVALID_ARG;
   }
   const bool q_same = p->q_stride_token == p->q_out_stride_token && p->q_stride_head == p->q_out_stride_head;
-  if (!written_apart(n_tiles, q_out, q, q_same)) return SG_ERR_INVALID_ARG;
+  const Written qw(q_out, n_tiles);
+  if (!qw.different() || !qw.apart_from(q, q_same)) return SG_ERR_INVALID_ARG;
   if (k) {
     const bool k_same = p->k_stride_token == p->k_out_stride_token && p->k_stride_head == p->k_out_stride_head;
-    if (!written_apart(n_tiles, k_out, k, k_same)) return SG_ERR_INVALID_ARG;
-    if (!written_apart(n_tiles, k_out, q, false) || !written_apart(n_tiles, q_out, k, false) ||
-        !written_apart(n_tiles, q_out, (const void* const*)k_out, false))
+    const Written kw(k_out, n_tiles);
+    if (!kw.different() || !kw.apart_from(k, k_same) || !kw.apart_from(q) || !qw.apart_from(k) || !qw.apart_from((const void* const*)k_out))
       return SG_ERR_INVALID_ARG;
   }
   return launch_rotary(*p, n_tiles, q, k, frequencies, origin, positions, q_weight, k_weight, run, q_out, k_out, (hipStream_t)stream);
@@ -169,15 +178,16 @@ int sg_tile_gated_norm(const sg_gated_norm_problem* p, int32_t n_tiles, const vo
     if (list && !tiles_ok(list, n_tiles)) return SG_ERR_INVALID_ARG;
   if (!aligned16(weight) || !aligned16(post_weight)) return SG_ERR_INVALID_ARG;
   if (eight != (out_scale != nullptr) || (eight && !tiles_ok((const void* const*)out_scale, n_tiles, 3u))) return SG_ERR_INVALID_ARG;
-  for (const void* const* list : {x, (const void* const*)residual, gate, scale, shift})
-    if (list && !written_apart(n_tiles, out, list, false)) return SG_ERR_INVALID_ARG;
+  const Written ow(out, n_tiles);
+  if (!ow.different() || !ow.apart_from(x)) return SG_ERR_INVALID_ARG;
+  for (const void* const* list : lists)
+    if (!ow.apart_from(list)) return SG_ERR_INVALID_ARG;
   if (sum) {
-    if (!tiles_ok((const void* const*)sum, n_tiles) || !written_apart(n_tiles, sum, x, p->x_stride == p->sum_stride) ||
-        (residual && !written_apart(n_tiles, sum, residual, p->residual_stride == p->sum_stride)) ||
-        !written_apart(n_tiles, out, (const void* const*)sum, false))
+    if (!tiles_ok((const void* const*)sum, n_tiles)) return SG_ERR_INVALID_ARG;
+    const Written sw(sum, n_tiles);
+    if (!sw.different() || !sw.apart_from(x, p->x_stride == p->sum_stride) || !sw.apart_from(residual, p->residual_stride == p->sum_stride) ||
+        !sw.apart_from(gate) || !sw.apart_from(scale) || !sw.apart_from(shift) || !ow.apart_from((const void* const*)sum))
       return SG_ERR_INVALID_ARG;
-    for (const void* const* list : {gate, scale, shift})
-      if (list && !written_apart(n_tiles, sum, list, false)) return SG_ERR_INVALID_ARG;
   }
   return launch_gated_norm(*p, n_tiles, x, residual, gate, post_weight, weight, scale, shift, run, sum, out, out_scale, (hipStream_t)stream);
 }
@@ -193,7 +203,8 @@ int sg_tile_int8_linear(const sg_int8_linear_problem* p, int32_t n_tiles, const 
   if (n_tiles == 0 || p->rows == 0) return SG_OK;
   if (!tiles_ok(x, n_tiles) || !tiles_ok((const void* const*)x_scale, n_tiles, 3u) || !tiles_ok((const void* const*)out, n_tiles)) return SG_ERR_INVALID_ARG;
   if (!w || !aligned16(w) || !w_scale || !aligned16(w_scale) || !aligned16(bias)) return SG_ERR_INVALID_ARG;
-  if (!written_apart(n_tiles, out, x, false)) return SG_ERR_INVALID_ARG;
+  const Written ow(out, n_tiles);
+  if (!ow.different() || !ow.apart_from(x)) return SG_ERR_INVALID_ARG;
   // rows are numbered in 31 bits; the largest calls are cut into blocks of 2^16 results, whose threads a grid has 2^32 of
   if ((int64_t)p->rows * n_tiles >= (1ll << 31) || (int64_t)p->rows * std::min(n_tiles, 64) >= (1ll << 39) / p->outputs) return SG_ERR_UNSUPPORTED;
   return launch_int8_linear(*p, n_tiles, x, x_scale, w, w_scale, bias, run, out, (hipStream_t)stream);

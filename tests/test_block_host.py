@@ -124,7 +124,7 @@ def test_binding_refuses_other_tensors():
     with pytest.raises(TypeError):
         sg.sg_tile_rotary(p, [t], [t], torch.zeros(32, dtype=torch.float64), positions=[torch.zeros(24, dtype=torch.int64)])
     with pytest.raises(TypeError):
-        sg.sg_tile_int8_linear(sg.make_int8_linear_problem(1, 16, 8, "f32"), [t.to(torch.uint8)], [], t.to(torch.int8), t, [t])
+        sg.sg_tile_int8_linear(sg.make_int8_linear_problem(1, 16, 8, "f32"), [t.to(torch.uint8)], [t], t.to(torch.int8), t, [t])
     with pytest.raises(TypeError):
         sg.sg_tile_int8_linear(sg.make_int8_linear_problem(1, 16, 8, "f32"), [t.to(torch.int8)], [t.double()], t.to(torch.int8), t, [t])
 
