@@ -8,12 +8,14 @@ namespace sg {
 template <typename T> struct Chan8;
 template <> struct Chan8<uint16_t> {
   u32x4 w;
+  __device__ __forceinline__ void clear() { w = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void load(const uint16_t* p) { w = *(const u32x4*)p; }
   __device__ __forceinline__ void stream(const uint16_t* p) { w = __builtin_nontemporal_load((const u32x4*)p); }   // rows that pass once
   __device__ __forceinline__ float get(int i) const { return i & 1 ? __uint_as_float(w[i >> 1] & 0xffff0000u) : __uint_as_float(w[i >> 1] << 16); }
 };
 template <> struct Chan8<float> {
   f32x4 a, b;
+  __device__ __forceinline__ void clear() { a = b = f32x4{0.f, 0.f, 0.f, 0.f}; }
   __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
   __device__ __forceinline__ void stream(const float* p) { load(p); }   // (the two halves of a lane's 32 bytes meet in the cache)
   __device__ __forceinline__ float get(int i) const { return i < 4 ? a[i] : b[i - 4]; }
