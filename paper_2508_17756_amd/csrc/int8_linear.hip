@@ -44,14 +44,6 @@ __device__ __forceinline__ float gelu(float v) {   // v (1 + tanh(u)) / 2 = v / 
   return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u));
 }
 
-__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
-  *(u32x4*)p = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-}
-__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
-  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-  *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-}
-
 // 8 outputs side by side of a row, from output o on.
 template <typename T> __device__ __forceinline__ void finish8(const LinearArgs& a, const int (&sum)[8], float x_scale, int o, T* out) {
   Chan8<float> ws;

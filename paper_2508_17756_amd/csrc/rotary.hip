@@ -3,8 +3,11 @@
 //
 // A workgroup takes a few tokens of a tile with all their heads (or a part of them): it computes the tokens' sines and cosines once, into LDS, and then
 // passes over the heads, each lane with 16 channels of one head as two vectors of 8 whose pairs lie in the lane.  The angle is a product in fp64
-// (positions reach millions of turns), reduced to a part of one turn there, and only that is rounded to fp32.  Bound by memory: every
-// channel is read and written once.
+// (positions reach millions of turns), reduced to a part of one turn there, and only that is rounded to fp32.
+//
+// Bound by memory, every channel read and written once: 75,600 tokens of 40 + 40 heads x 128 in bf16, token-major 570 us (5.4 TB/s; a large copy runs at 4.9), with
+// the norm of the heads 585, head-major 625 - 640; 9 x 4,000 tokens of 40 + 8 heads 172 us (5.1).  Few short heads are bound by the sines: 9 tiles of 75,600
+// tokens, 1 + 1 heads x 64 100 us (3.5 TB/s).
 #include "block_api.h"
 #include "row_common.h"
 
@@ -38,7 +41,7 @@ struct RotaryArgs {
   float eps;
 };
 
-template <typename T, bool HALF>
+template <typename T, bool HALF, bool LINES>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const RotaryTable tab) {
   extern __shared__ float turns[];   // [chunk][pairs padded to 8] cosines, then sines
   const int tile = (int)divide(blockIdx.x, a.by_chunks);
@@ -48,29 +51,6 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const R
   const int pairs = a.turned >> 1, row_pairs = (pairs + 7) & ~7;
   float* const cosines = turns;
   float* const sines = turns + a.chunk * row_pairs;
-
-  for (int i = threadIdx.x; i < n_tokens * row_pairs; i += 256) {
-    const int t = i / row_pairs, pair = i - t * row_pairs;
-    if (pair >= pairs) continue;
-    const int token = token0 + t;
-    const int axis = (pair >= a.first_y) + (pair >= a.first_x);
-    int position;
-    if (tab.positions[tile]) {
-      position = a.position_axes == 1 ? tab.positions[tile][token] : tab.positions[tile][3 * (int64_t)token + axis];
-    } else {
-      const int frame = (int)divide((uint32_t)token, a.by_plane), rest = token - frame * a.H_W;
-      const int y = (int)divide((uint32_t)rest, a.by_row);
-      position = tab.origin[tile][axis] + (axis == 0 ? frame : axis == 1 ? y : rest - y * a.W);
-      if (a.canvas[axis] > 0) position = (int)((uint32_t)position % (uint32_t)a.canvas[axis]);   // (the origin lies inside the canvas)
-    }
-    double turn = (double)position * (a.frequencies[pair] * 0.15915494309189535);   // 1 / (2 pi)
-    turn -= __builtin_rint(turn);
-    float sine, cosine;
-    sincospif(2.f * (float)turn, &sine, &cosine);
-    cosines[i] = cosine;
-    sines[i] = sine;
-  }
-  __syncthreads();
 
   const int head0 = blockIdx.y * a.head_step;
   const int n_heads = a.all_heads - head0 < a.head_step ? a.all_heads - head0 : a.head_step;
@@ -88,7 +68,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const R
     vb = l + (a.n_vec + 1) / 2;
   }
   const bool has_b = has_a && vb < a.n_vec;
-  for (int r = threadIdx.x >> a.lane_shift; r < n_rows; r += 256 >> a.lane_shift) {
+  struct Row { int t, head; };
+  auto row_of = [&](int r) {
     int t, head;
     if (a.by_token) {
       t = n_heads == a.all_heads ? (int)divide((uint32_t)r, a.by_heads) : r / n_heads;
@@ -97,30 +78,74 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const R
       head = n_tokens == a.chunk ? r >> a.chunk_shift : r / n_tokens;
       t = r - head * n_tokens;
     }
-    head += head0;
-    const bool is_k = head >= a.heads;
-    const int64_t token = token0 + t;
-    const T* x;
-    T* y;
-    const T* weight;
-    if (is_k) {
-      const int h = head - a.heads;
-      x = (const T*)tab.k[tile] + token * a.k_token + h * a.k_head;
-      y = (T*)tab.k_out[tile] + token * a.ko_token + h * a.ko_head;
-      weight = (const T*)a.k_weight;
+    return Row{t, head + head0};
+  };
+  const T* const q = (const T*)tab.q[tile] + token0 * a.q_token;
+  const T* const k = (const T*)tab.k[tile] + token0 * a.k_token;   // (from here on offsets of the workgroup's tokens)
+  T* const q_out = (T*)tab.q_out[tile] + token0 * a.qo_token;
+  T* const k_out = (T*)tab.k_out[tile] + token0 * a.ko_token;
+  Chan8<T> ra, rb;
+  auto fetch = [&](Row w) {
+    const T* const x = w.head >= a.heads ? k + w.t * a.k_token + (w.head - a.heads) * a.k_head : q + w.t * a.q_token + w.head * a.q_head;
+    if constexpr (LINES) {
+      if (has_a) ra.stream(x + 8 * va);
+      if (has_b) rb.stream(x + 8 * vb);
     } else {
-      x = (const T*)tab.q[tile] + token * a.q_token + head * a.q_head;
-      y = (T*)tab.q_out[tile] + token * a.qo_token + head * a.qo_head;
-      weight = (const T*)a.q_weight;
+      if (has_a) ra.load(x + 8 * va);
+      if (has_b) rb.load(x + 8 * vb);
     }
-    Chan8<T> ra, rb;
-    if (has_a) ra.stream(x + 8 * va);
-    if (has_b) rb.stream(x + 8 * vb);
+  };
+  // The first rows are on their way while the sines are computed, the next ones while a row is turned.
+  const int step = 256 >> a.lane_shift;
+  int r = threadIdx.x >> a.lane_shift;
+  Row now = row_of(r < n_rows ? r : 0);
+  if (r < n_rows) fetch(now);
+
+  for (int i = threadIdx.x; i < n_tokens * row_pairs; i += 256) {
+    const int t = i / row_pairs, pair = i - t * row_pairs;
+    if (pair >= pairs) continue;
+    const int token = token0 + t;
+    const int axis = (pair >= a.first_y) + (pair >= a.first_x);
+    int position;
+    if (tab.positions[tile]) {
+      position = a.position_axes == 1 ? tab.positions[tile][token] : tab.positions[tile][3 * (int64_t)token + axis];
+    } else {
+      const int frame = (int)divide((uint32_t)token, a.by_plane), rest = token - frame * a.H_W;
+      const int y = (int)divide((uint32_t)rest, a.by_row);
+      const int* const origin = tab.origin[tile];
+      position = axis == 0 ? origin[0] + frame : axis == 1 ? origin[1] + y : origin[2] + rest - y * a.W;
+      const int size = axis == 0 ? a.canvas[0] : axis == 1 ? a.canvas[1] : a.canvas[2];
+      if (size > 0) position = (int)((uint32_t)position % (uint32_t)size);   // (the origin lies inside the canvas)
+    }
+    double turn = (double)position * (a.frequencies[pair] * 0.15915494309189535);   // 1 / (2 pi)
+    turn -= __builtin_rint(turn);
+    float sine, cosine;
+    if constexpr (sizeof(T) == 2) {   // the instructions take parts of a turn and are off by 2^-22.9 at most over one (measured; sincospif in the fp32 form: 2^-24)
+      sine = __builtin_amdgcn_sinf((float)turn);
+      cosine = __builtin_amdgcn_cosf((float)turn);
+    } else {
+      sincospif(2.f * (float)turn, &sine, &cosine);
+    }
+    cosines[i] = cosine;
+    sines[i] = sine;
+  }
+  __syncthreads();
+
+  for (; r < n_rows;) {
     float u[8], v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       u[e] = has_a ? ra.get(e) : 0.f;
       v[e] = has_b ? rb.get(e) : 0.f;
+    }
+    const int t = now.t;
+    const bool is_k = now.head >= a.heads;
+    const T* const weight = (const T*)(is_k ? a.k_weight : a.q_weight);
+    T* const y = is_k ? k_out + t * a.ko_token + (now.head - a.heads) * a.ko_head : q_out + t * a.qo_token + now.head * a.qo_head;
+    r += step;
+    if (r < n_rows) {
+      now = row_of(r);
+      fetch(now);
     }
     if (a.q_weight || a.k_weight) {   // (the lanes of a row agree on `weight`)
       float sq = 0.f;
@@ -174,8 +199,13 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const R
         }
       }
     }
-    if (has_a) stream8(y + 8 * va, u);
-    if (has_b) stream8(y + 8 * vb, v);
+    if constexpr (LINES) {
+      if (has_a) stream8(y + 8 * va, u);
+      if (has_b) stream8(y + 8 * vb, v);
+    } else {
+      if (has_a) store8(y + 8 * va, u);
+      if (has_b) store8(y + 8 * vb, v);
+    }
   }
 }
 
@@ -201,10 +231,15 @@ int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q,
   a.by_heads = make_divisor((uint32_t)a.all_heads);
   a.by_token = p.q_stride_head < p.q_stride_token;
   a.eps = p.eps;
-  // Tokens of a workgroup: enough rows for 8 passes of it, its table within 32 KiB.
+  // Tokens of a workgroup: rows for one pass of it at least and 8 at most, where that leaves 2,048 workgroups (2 x 36 x 40 tokens, 4 tiles, 8 + 8 heads of 128,
+  // fp32: 45 us, with 8 passes 49); heads that lie apart: for runs of 4 KiB, up to 64 passes (75,600 tokens 640 us, with 8 662).  Its table within 32 KiB.
   const int rows_per_pass = 256 >> a.lane_shift, row_pairs = (a.turned / 2 + 7) & ~7;
+  const int passes_most = a.by_token ? 8 : 64;
+  const int run_bytes = p.head_dim * (p.dtype == SG_F32 ? 4 : 2);
   a.chunk = 1; a.chunk_shift = 0;
-  while (a.chunk < 64 && a.chunk < a.tokens && (int64_t)a.chunk * a.all_heads < 8 * rows_per_pass && 2 * a.chunk * row_pairs * 8 <= 32768) {
+  while (a.chunk < 64 && a.chunk < a.tokens && 2 * a.chunk * row_pairs * 8 <= 32768) {
+    const int64_t rows = (int64_t)a.chunk * a.all_heads, wgs = (int64_t)n_tiles * a.tokens / (2 * a.chunk);
+    if (rows >= rows_per_pass && (wgs < 2048 || rows >= passes_most * rows_per_pass || (rows >= 8 * rows_per_pass && a.chunk * run_bytes >= 4096))) break;
     a.chunk <<= 1; ++a.chunk_shift;
   }
   a.chunks = (a.tokens + a.chunk - 1) / a.chunk;
@@ -234,13 +269,21 @@ int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q,
     a.head_step = (a.all_heads + splits - 1) / splits;
     splits = (a.all_heads + a.head_step - 1) / a.head_step;
     const dim3 grid((unsigned)wgs, (unsigned)splits);
+    // Where a load of a head's lanes takes whole cache lines, they pass the caches by; other heads' lines are met twice (4 tiles of 75,600 tokens, 5 + 5 heads
+    // x 96 309 us, past the caches 356).
+    const bool half = p.layout == SG_ROTARY_HALF, lines = p.head_dim % 128 == 0;
+#define SG_ROTARY(T, H, L) rotary_kernel<T, H, L><<<grid, 256, lds, s>>>(a, tab)
     if (p.dtype == SG_F32) {
-      if (p.layout == SG_ROTARY_HALF) rotary_kernel<float, true><<<grid, 256, lds, s>>>(a, tab);
-      else rotary_kernel<float, false><<<grid, 256, lds, s>>>(a, tab);
+      if (half) SG_ROTARY(float, true, false);
+      else SG_ROTARY(float, false, false);
+    } else if (lines) {
+      if (half) SG_ROTARY(uint16_t, true, true);
+      else SG_ROTARY(uint16_t, false, true);
     } else {
-      if (p.layout == SG_ROTARY_HALF) rotary_kernel<uint16_t, true><<<grid, 256, lds, s>>>(a, tab);
-      else rotary_kernel<uint16_t, false><<<grid, 256, lds, s>>>(a, tab);
+      if (half) SG_ROTARY(uint16_t, true, false);
+      else SG_ROTARY(uint16_t, false, false);
     }
+#undef SG_ROTARY
     SG_HIP_TRY(hipGetLastError());
   }
   return SG_OK;

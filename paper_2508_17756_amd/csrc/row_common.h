@@ -28,6 +28,11 @@ __device__ __forceinline__ void stream8(float* p, const float (&v)[8]) {
   *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
 
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+  *(u32x4*)p = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) { stream8(p, v); }
+
 // The larger of two numbers; NaN where one is.
 __device__ __forceinline__ float larger_or_nan(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
