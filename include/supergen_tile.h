@@ -650,7 +650,7 @@ typedef enum { SG_ACT_NONE = 0, SG_ACT_GELU = 1 } sg_activation;
 typedef struct sg_int8_linear_problem {
   int32_t rows;               /* tokens of a tile, >= 0                                                          */
   int32_t channels;           /* inputs: a multiple of 16, 16 .. 131056                                          */
-  int32_t outputs;            /* a multiple of 8, >= 8                                                           */
+  int32_t outputs;            /* a multiple of 8, 8 .. 2^26                                                      */
   int32_t dtype;              /* SG_F32 or SG_BF16: bias and out                                                  */
   int32_t activation;         /* sg_activation                                                                   */
   int64_t x_stride, w_stride; /* between rows, in elements: multiples of 16, >= channels                         */
@@ -670,7 +670,8 @@ int sg_int8_linear_validate(const sg_int8_linear_problem* p);
  *   out        host array of device pointers: rows of outputs in dtype; alias nothing
  * The sum is one of integers in 32 bits and exact (-128 too); it is rounded to fp32 and scaled there, first by the token's, then by the output's factor, and the
  * result is rounded once.  GELU is v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2.  A token or output whose scale is NaN gives NaN, and no other does.
- * Tensors are 16-byte aligned (x_scale: 4).  rows * n_tiles is below 2^31, rows * outputs of 64 tiles below 2^39.
+ * Tensors are 16-byte aligned (x_scale: 4).  w_scale: 16-byte aligned too.  rows * n_tiles is below 2^31, and 64 tiles have less than 2^23 blocks of 256 rows x 256
+ * outputs, ends counted as whole ones.
  */
 int sg_tile_int8_linear(const sg_int8_linear_problem* p, int32_t n_tiles, const void* const* x, const float* const* x_scale, const void* w,
                         const float* w_scale, const void* bias, const uint8_t* run, void* const* out, void* stream);

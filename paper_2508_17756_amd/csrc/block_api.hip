@@ -83,7 +83,7 @@ static int validate(const sg_int8_linear_problem* p) {
   if (p->activation != SG_ACT_NONE && p->activation != SG_ACT_GELU) return SG_ERR_INVALID_ARG;
   if (!row_stride_ok(p->x_stride, p->channels, 16) || !row_stride_ok(p->w_stride, p->channels, 16) || !row_stride_ok(p->out_stride, p->outputs, 8))
     return SG_ERR_INVALID_ARG;
-  if (p->channels > 131056) return SG_ERR_UNSUPPORTED;
+  if (p->channels > 131056 || p->outputs > (1 << 26)) return SG_ERR_UNSUPPORTED;
   return SG_OK;
 }
 
@@ -205,8 +205,9 @@ int sg_tile_int8_linear(const sg_int8_linear_problem* p, int32_t n_tiles, const 
   if (!w || !aligned16(w) || !w_scale || !aligned16(w_scale) || !aligned16(bias)) return SG_ERR_INVALID_ARG;
   const Written ow(out, n_tiles);
   if (!ow.different() || !ow.apart_from(x)) return SG_ERR_INVALID_ARG;
-  // rows are numbered in 31 bits; the largest calls are cut into blocks of 2^16 results, whose threads a grid has 2^32 of
-  if ((int64_t)p->rows * n_tiles >= (1ll << 31) || (int64_t)p->rows * std::min(n_tiles, 64) >= (1ll << 39) / p->outputs) return SG_ERR_UNSUPPORTED;
+  // rows are numbered in 31 bits; the largest calls are cut into blocks of 256 x 256, a workgroup of 512 threads each, for 64 tiles a launch
+  const int64_t rows = (int64_t)p->rows * std::min(n_tiles, 64);
+  if ((int64_t)p->rows * n_tiles >= (1ll << 31) || (rows + 255) / 256 * ((p->outputs + 255ll) / 256) >= (1ll << 23)) return SG_ERR_UNSUPPORTED;
   return launch_int8_linear(*p, n_tiles, x, x_scale, w, w_scale, bias, run, out, (hipStream_t)stream);
 }
 

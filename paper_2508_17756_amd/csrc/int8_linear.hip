@@ -249,8 +249,9 @@ __global__ __launch_bounds__(64 * WAVES) void int8_linear_rows_kernel(const Line
   __shared__ int sums[16 * MT * kPitch];          // [row][output]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t total = (uint32_t)running_tiles(a, list) * (uint32_t)a.rows;
-  const uint32_t m0 = blockIdx.y * 16 * MT;
-  const int n0 = blockIdx.x * 16 * NT;
+  const uint32_t blocks_n = (uint32_t)(a.outputs + 16 * NT - 1) / (16 * NT), m = blockIdx.x / blocks_n;
+  const uint32_t m0 = m * 16 * MT;
+  const int n0 = (int)(blockIdx.x - m * blocks_n) * 16 * NT;
   if (m0 >= total) return;
   const int stages = (a.channels + BK - 1) / BK, n = (stages - wave + WAVES - 1) / WAVES;   // of the wavefront: stage k WAVES + wave
   const char* from[kLoads];
@@ -363,7 +364,7 @@ int launch(LinearArgs& a, const LinearTable& tab, hipStream_t s) {
 
 template <typename T, int MT, int NT, int DEPTH, int WAVES> int launch_rows(const LinearArgs& a, const LinearTable& tab, hipStream_t s) {
   const int64_t rows = (int64_t)a.n_tiles * a.rows;
-  const dim3 grid((unsigned)((a.outputs + 16 * NT - 1) / (16 * NT)), (unsigned)((rows + 16 * MT - 1) / (16 * MT)));
+  const dim3 grid((unsigned)(((a.outputs + 16 * NT - 1) / (16 * NT)) * ((rows + 16 * MT - 1) / (16 * MT))));
   constexpr size_t kLds = WAVES * DEPTH * 16 * (MT + NT) * 128;
   static std::atomic<bool> raised[kMaxDevices];
   auto* const kernel = int8_linear_rows_kernel<T, MT, NT, DEPTH, WAVES>;
@@ -388,9 +389,11 @@ template <typename T> int launch_best(LinearArgs& a, const LinearTable& tab, hip
   const int64_t b256 = blocks(256, 256), b128 = blocks(128, 128), b64 = blocks(64, 64), b32 = blocks(32, 32);
   const int64_t t256 = (b256 + 255) / 256 * 68000, t128 = b128 <= 256 ? 42000 : (b128 + 511) / 512 * 46000, t64 = b64 <= 256 ? 19000 : 10000 + 36 * b64,
                 t32 = 8000 + 15 * b32;
-  if (t32 <= t64 && t32 <= t128 && t32 <= t256) return launch_rows<T, 2, 2, 2, 4>(a, tab, s);
-  if (t64 <= t128 && t64 <= t256) return launch<T, 64, 64, 2, 2, 3>(a, tab, s);
-  if (t128 <= t256) return launch<T, 128, 128, 2, 2, 2>(a, tab, s);
+  // (a grid has less than 2^32 threads: 256 of a workgroup, 512 of the largest blocks, whose number the call's checks bound)
+  constexpr int64_t kMost = (1ll << 24) - 1;
+  if (b32 <= kMost && t32 <= t64 && t32 <= t128 && t32 <= t256) return launch_rows<T, 2, 2, 2, 4>(a, tab, s);
+  if (b64 <= kMost && t64 <= t128 && t64 <= t256) return launch<T, 64, 64, 2, 2, 3>(a, tab, s);
+  if (b128 <= kMost && t128 <= t256) return launch<T, 128, 128, 2, 2, 2>(a, tab, s);
   return launch<T, 256, 256, 2, 4, 2>(a, tab, s);
 }
 

@@ -245,8 +245,11 @@ int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q,
   a.chunks = (a.tokens + a.chunk - 1) / a.chunk;
   a.by_chunks = make_divisor((uint32_t)a.chunks);
   const size_t lds = (size_t)a.chunk * row_pairs * 8;
-  for (int t0 = 0; t0 < n_tiles; t0 += kRotaryTilesPerLaunch) {
-    const int n = n_tiles - t0 < kRotaryTilesPerLaunch ? n_tiles - t0 : kRotaryTilesPerLaunch;
+  // A grid has less than 2^32 threads: 2^24 workgroups, times the parts of few tokens' heads.
+  int most_tiles = ((1 << 24) - 1) / a.chunks;
+  most_tiles = most_tiles < 1 ? 1 : most_tiles > kRotaryTilesPerLaunch ? kRotaryTilesPerLaunch : most_tiles;
+  for (int t0 = 0; t0 < n_tiles; t0 += most_tiles) {
+    const int n = n_tiles - t0 < most_tiles ? n_tiles - t0 : most_tiles;
     RotaryTable tab = {};
     for (int i = 0; i < n; ++i) {
       tab.q[i] = q[t0 + i];

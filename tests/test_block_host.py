@@ -177,7 +177,8 @@ def test_gated_norms_that_are_not(kw):
     ({}, sg.SG_OK), ({"rows": 0}, sg.SG_OK), ({"rows": -1}, BAD), ({"channels": 0}, BAD), ({"channels": 72}, BAD), ({"outputs": 0}, BAD), ({"outputs": 12}, BAD),
     ({"dtype": 2}, BAD), ({"dtype": 3}, BAD), ({"activation": 2}, BAD), ({"activation": -1}, BAD), ({"x_stride": 48}, BAD), ({"x_stride": 72}, BAD), ({"w_stride": 0}, BAD),
     ({"out_stride": 32}, BAD), ({"out_stride": 44}, BAD), ({"x_stride": 1 << 40}, BAD), ({"channels": 131072, "x_stride": 131072, "w_stride": 131072}, NO),
-    ({"channels": 131056, "x_stride": 131056, "w_stride": 131056}, sg.SG_OK)])
+    ({"channels": 131056, "x_stride": 131056, "w_stride": 131056}, sg.SG_OK), ({"outputs": 1 << 26, "out_stride": 1 << 26}, sg.SG_OK),
+    ({"outputs": (1 << 26) + 8, "out_stride": (1 << 26) + 8}, NO)])
 def test_linear_problem_is_checked(fields, status):
     p = sg.make_int8_linear_problem(6, 64, 40, "bf16")
     for name, value in fields.items():
@@ -198,12 +199,15 @@ def _linear(n=2, fields=None, **kw):
     (dict(n=0), sg.SG_OK), (dict(fields={"rows": 0}), sg.SG_OK), (dict(n=-1, x=None), BAD), (dict(n=257), NO), (dict(x=None), BAD), (dict(x_scale=None), BAD), (dict(out=None), BAD),
     (dict(w=None), BAD), (dict(w_scale=None), BAD), (dict(w=GOOD + 8), BAD), (dict(w_scale=GOOD + 4), BAD), (dict(bias=GOOD + 2), BAD), (dict(x=_at(2, 0, 8)), BAD),
     (dict(x_scale=_at(2, 300, 2)), BAD), (dict(out=_at(2, 600, 4)), BAD), (dict(out=_at(2)), BAD), (dict(out=_list([600, 600])), BAD),
-    (dict(fields={"rows": 1 << 30}), NO), (dict(fields={"rows": 1 << 20, "outputs": 1 << 19, "out_stride": 1 << 19}), NO)])
+    (dict(fields={"rows": 1 << 30}), NO), (dict(fields={"rows": 1 << 20, "outputs": 1 << 19, "out_stride": 1 << 19}), NO),
+    (dict(fields={"outputs": (1 << 26) + 8, "out_stride": (1 << 26) + 8}), NO), (dict(fields={"rows": 257, "outputs": 1 << 26, "out_stride": 1 << 26}, n=64), NO)])
 def test_linear_calls_are_refused(kw, status):
     assert _linear(**kw) == status
 
 
 @no_device
-@pytest.mark.parametrize("kw", [{}, dict(bias=None), dict(x=_list([0, 0])), dict(x_scale=_at(2, 300, 4)), dict(fields={"rows": 1 << 20, "outputs": 1 << 16, "out_stride": 1 << 16})])
+@pytest.mark.parametrize("kw", [{}, dict(bias=None), dict(x=_list([0, 0])), dict(x_scale=_at(2, 300, 4)), dict(fields={"rows": 1 << 20, "outputs": 1 << 16, "out_stride": 1 << 16}),
+                                dict(fields={"rows": (1 << 29) - 1}), dict(n=1, fields={"rows": 1, "outputs": 1 << 26, "out_stride": 1 << 26}),
+                                dict(n=1, fields={"rows": 64, "outputs": 1 << 26, "out_stride": 1 << 26})])
 def test_linear_calls_that_are_not(kw):
     assert _linear(**kw) == DONE
