@@ -44,6 +44,9 @@ __device__ __forceinline__ float gelu(float v) {   // v (1 + tanh(u)) / 2 = v / 
   return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u));
 }
 
+__device__ __forceinline__ float to_float(uint16_t v) { return bf16_bits_to_f32(v); }
+__device__ __forceinline__ float to_float(float v) { return v; }
+
 // 8 outputs side by side of a row, from output o on.
 template <typename T> __device__ __forceinline__ void finish8(const LinearArgs& a, const int (&sum)[8], float x_scale, int o, T* out) {
   Chan8<float> ws;
@@ -70,14 +73,14 @@ __device__ __forceinline__ int running_tiles(const LinearArgs& a, int* list) {
   return __popcll(mask);
 }
 
-// Workgroups go to the 8 XCDs in turn: each XCD takes a run of blocks, in columns of up to 8 blocks of rows, so that the 32 that run on it side by
-// side share 8 parts of x and 4 of w in its L2.
+// Workgroups go to the 8 XCDs in turn: each XCD takes a run of blocks, in columns of up to 4 blocks of rows, so that the 32 that run on it side by
+// side share 4 parts of x and 8 of w in its L2 (75,600 x 5,120 x 20,480: 6.77 ms; columns of 8 6.95, of 16 7.10).
 __device__ __forceinline__ void block_of(uint32_t id, uint32_t gm, uint32_t gn, uint32_t& m, uint32_t& n) {
   const uint32_t all = gm * gn, xcd = id & 7, per = all >> 3, more = all & 7;
   const uint32_t at = xcd * per + (xcd < more ? xcd : more) + (id >> 3);
-  const uint32_t group = at / (8 * gn), rest = at - group * 8 * gn, left = gm - group * 8, tall = left < 8 ? left : 8;
+  const uint32_t group = at / (4 * gn), rest = at - group * 4 * gn, left = gm - group * 4, tall = left < 4 ? left : 4;
   n = rest / tall;
-  m = group * 8 + rest - n * tall;
+  m = group * 4 + rest - n * tall;
 }
 
 template <typename T, int BM, int BN, int WM, int WN, int STAGES>
@@ -88,6 +91,10 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
   static_assert(kRows % (8 * kWaves) == 0 && kWaves % 2 == 0 && FM * WM * 16 == BM && FN * WN * 16 == BN && FM % 2 == 0 && FN % 2 == 0, "tiles");
   static_assert((STAGES + 1) * BK + 16 <= (int)sizeof(kNoChannels) && kAhead + kLoads < 64, "loads behind the end, loads in flight");
   extern __shared__ __align__(1024) char lds[];   // [STAGES][BM rows of x, BN rows of w][BK]
+  struct Row { const char* x; T* out; };
+  __shared__ Row rows[BM];
+  __shared__ float x_scales[BM];
+  __shared__ __align__(16) float w_scales[BN], biases[BN];
   __shared__ int list[kLinearTilesPerLaunch];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t total = (uint32_t)running_tiles(a, list) * (uint32_t)a.rows;
@@ -103,16 +110,32 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
     return (int64_t)(r - i * (uint32_t)a.rows);
   };
 
+  // A thread finds the place of one row, for all that load or store it, and brings a row's and an output's factors for the end.
+  static_assert(64 * kWaves >= BM && 64 * kWaves >= BN, "a row and an output a thread");
+  float row_scale = 0.f, out_scale = 0.f, out_bias = 0.f;
+  if (threadIdx.x < BM) {
+    int tile;
+    const int64_t at = row_at(m0 + threadIdx.x, tile);
+    rows[threadIdx.x] = {(const char*)tab.x[tile] + at * a.x_stride, (T*)tab.out[tile] + at * a.o_stride};
+    row_scale = tab.x_scale[tile][at];
+  }
+  if (threadIdx.x < BN) {
+    const int o = n0 + (int)threadIdx.x < a.outputs ? n0 + (int)threadIdx.x : a.outputs - 1;
+    out_scale = a.w_scale[o];
+    if (a.bias) out_bias = to_float(((const T*)a.bias)[o]);
+  }
+  __syncthreads();
+
   // One 1 KiB piece of a stage, 8 rows, is a load of a wavefront: lane i fills the i-th 16 bytes.
   const char* from[kLoads];
   const int channel = 16 * ((lane & 7) ^ ((wave & 1) << 2 | lane >> 4));
+  constexpr int kXLoads = BM / (8 * kWaves);
+  static_assert(BM % (8 * kWaves) == 0, "a piece has rows of x or of w");
 #pragma unroll
   for (int j = 0; j < kLoads; ++j) {
     const int row = (wave + j * kWaves) * 8 + (lane >> 3);
-    if (row < BM) {
-      int tile;
-      const int64_t at = row_at(m0 + row, tile);
-      from[j] = (const char*)tab.x[tile] + at * a.x_stride + channel;
+    if (j < kXLoads) {
+      from[j] = rows[row].x + channel;
     } else {
       // Row 16 i + r of a wavefront's outputs is output 4 FN (r / 4) + 4 i + r mod 4 of them: what a lane gets is then side by side.
       const int w = (row - BM) % (16 * FN), r = w & 15;
@@ -139,11 +162,12 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
   i32x4 acc[FN][FM] = {}, xf[FM], wf[2][FN];
   const int wm = wave % WM, wn = wave / WM;
   const int r16 = lane & 15, quarter = lane >> 4;
-  auto at = [&](int buffer, int c, int row) {   // what the lane gives of 16 rows at step c
-    return (const i32x4*)(lds + buffer * kStageBytes + (row + r16) * BK + 16 * ((4 * c + quarter) ^ (r16 >> 1)));
-  };
-  auto read_x = [&](int buffer, int c, int j) { xf[j] = *at(buffer, c, (wm * FM + j) * 16); };
-  auto read_w = [&](int buffer, int c, int i) { wf[c][i] = *at(buffer, c, BM + (wn * FN + i) * 16); };
+  // What the lane gives of 16 rows at steps 0 and 1.
+  const char* const at[2] = {lds + r16 * BK + 16 * (quarter ^ (r16 >> 1)), lds + r16 * BK + 16 * ((4 + quarter) ^ (r16 >> 1))};
+  const char* const x_at[2] = {at[0] + wm * FM * 16 * BK, at[1] + wm * FM * 16 * BK};
+  const char* const w_at[2] = {at[0] + (BM + wn * FN * 16) * BK, at[1] + (BM + wn * FN * 16) * BK};
+  auto read_x = [&](int buffer, int c, int j) { xf[j] = *(const i32x4*)(x_at[c] + buffer * kStageBytes + j * 16 * BK); };
+  auto read_w = [&](int buffer, int c, int i) { wf[c][i] = *(const i32x4*)(w_at[c] + buffer * kStageBytes + i * 16 * BK); };
   // Group j of step c; what `between` reads or loads goes out in the shadow of its products.
   auto group = [&](int c, int j, auto between) {
     __builtin_amdgcn_sched_barrier(0);
@@ -214,25 +238,33 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
   for (int j = FM / 2; j < FM; ++j) group(1, j, [] {});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing arrives in LDS that is another workgroup's by then
 
+  if (threadIdx.x < BM) x_scales[threadIdx.x] = row_scale;
+  if (threadIdx.x < BN) { w_scales[threadIdx.x] = out_scale; biases[threadIdx.x] = out_bias; }
+  __syncthreads();
+
   // Lane: row r16 of each 16 rows; 4 FN outputs side by side.
-  const int o0 = n0 + (wn * 4 + quarter) * 4 * FN;
-  if (o0 >= a.outputs) return;
+  const int o_in = (wn * 4 + quarter) * 4 * FN;
+  Chan8<float> ws[FN / 2], bs[FN / 2];
+#pragma unroll
+  for (int i = 0; i < FN / 2; ++i) {
+    ws[i].load(w_scales + o_in + 8 * i);
+    bs[i].load(biases + o_in + 8 * i);
+  }
 #pragma unroll
   for (int j = 0; j < FM; ++j) {
-    const uint32_t r = m0 + (wm * FM + j) * 16 + r16;
-    if (r >= total) continue;
-    int tile;
-    const int64_t row = row_at(r, tile);
-    const float xs = tab.x_scale[tile][row];
-    T* const out = (T*)tab.out[tile] + row * a.o_stride;
+    const int row = (wm * FM + j) * 16 + r16;
+    const float xs = x_scales[row];
+    T* const out = rows[row].out + n0 + o_in;
 #pragma unroll
     for (int i = 0; i < FN; i += 2) {
-      const int o = o0 + 4 * i;
-      if (o >= a.outputs) continue;
-      int v[8];
+      float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = acc[i + e / 4][j][e % 4];
-      finish8<T>(a, v, xs, o, out + o);
+      for (int e = 0; e < 8; ++e) {
+        v[e] = (float)acc[i + e / 4][j][e % 4] * xs;
+        v[e] = a.bias ? fmaf(v[e], ws[i / 2].get(e), bs[i / 2].get(e)) : v[e] * ws[i / 2].get(e);
+        if (a.gelu) v[e] = gelu(v[e]);
+      }
+      if (m0 + row < total && n0 + o_in + 4 * i < a.outputs) store8(out + 4 * i, v);
     }
   }
 }
