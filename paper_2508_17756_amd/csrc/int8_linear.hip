@@ -6,9 +6,11 @@
 // are stored in the order piece ^ (row / 2 mod 8): 16 lanes that read the same piece of 16 rows then meet 16 different groups of the 64 banks.
 // w is the instruction's first operand, its rows in an order that leaves a lane with outputs side by side of one row, which it scales and stores together.
 //
-// Large calls are bound by the power that the products take: held in registers, N(0, 32)-distributed integers pass the instruction at 3.9 POP/s (zeros: 4.9;
-// the form 32x32x32, which touches each sum twice as often, at 3.3).  Blocks of 256 x 256: 34,560 x 5,120 x 15,360 2.35 ms = 2.31 POP/s (with 32x32x32: 2.58),
-// 75,600 x 5,120 x 20,480 with GELU 7.1 - 7.4 ms = 2.14 - 2.22 POP/s; on zeros the former takes 2.07.
+// Large calls: held in registers, N(0, 32)-distributed integers pass the instruction at 3.9 POP/s, bound by power (zeros: 4.9; the form 32x32x32, which touches each
+// sum twice as often, at 3.3).  Blocks of 256 x 256: 34,560 x 5,120 x 15,360 2.19 ms = 2.48 POP/s, 75,600 x 5,120 x 20,480 with GELU 6.7 - 6.8 ms = 2.33 - 2.37.  A
+// block's 40 stages take seven eighths of its time, the matrix pipe busy for 0.7 of them: what is lost there is the barrier of each stage, where the two
+// wavefronts of a SIMD leave it empty, and in the last eighth its start and its stores.  32x32x32 instead: 2.58 ms at the first size; all of a stage's loads
+// behind its barrier: 2.23; factors and places of the rows looked up at the end: 2.35.
 #include <atomic>
 #include "block_api.h"
 #include "row_common.h"
@@ -182,14 +184,21 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
     }
     __builtin_amdgcn_sched_barrier(0);
   };
-  constexpr int kReads = (FN + FM - 1) / FM;
-  auto first_step = [&](int buffer) {
+  // The loads of a stage go out beside the second half of one step's groups and all of the next one's.
+  constexpr int kHalf = FM / 2, kReads = (FN + FM - 1) / FM, kLoadsPer = (kLoads + kHalf + FM - 1) / (kHalf + FM);
+  auto load_some = [&](int group, int buffer) {
+#pragma unroll
+    for (int l = group * kLoadsPer; l < (group + 1) * kLoadsPer; ++l)
+      if (l < kLoads) load(l, buffer);
+  };
+  auto first_step = [&](int buffer, int read_out) {   // read_out: a buffer that is to be filled, or -1
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
       group(0, j, [&] {
 #pragma unroll
         for (int i = j * kReads; i < (j + 1) * kReads; ++i)
           if (i < FN) read_w(buffer, 1, i);
+        if (read_out >= 0) load_some(kHalf + j, read_out);
       });
       read_x(buffer, 1, j);
     }
@@ -205,9 +214,9 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
   for (int i = 0; i < FN; ++i) read_w(0, 0, i);
 #pragma unroll
   for (int j = 0; j < FM; ++j) read_x(0, 0, j);
-  first_step(0);
+  first_step(0, -1);
 #pragma unroll
-  for (int j = 0; j < FM / 2; ++j) group(1, j, [] {});
+  for (int j = 0; j < kHalf; ++j) group(1, j, [] {});
   // The barrier stands in the middle of the second step: by then every read of the stage has long been issued, and the other half of the products covers
   // the first reads of the next stage.
   int buffer = 0;
@@ -215,7 +224,7 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
     const int next = buffer + 1 == STAGES ? 0 : buffer + 1;
     check_end(k + STAGES);
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(kAhead) : "memory");
-    constexpr int kHalf = FM / 2, kLoadsPer = (kLoads + kHalf - 1) / kHalf, kWPer = (FN + kHalf - 1) / kHalf;
+    constexpr int kWPer = (FN + kHalf - 1) / kHalf;
 #pragma unroll
     for (int j = 0; j < kHalf; ++j) {
       group(1, kHalf + j, [&] {
@@ -223,19 +232,18 @@ __global__ __launch_bounds__(64 * WM * WN) void int8_linear_kernel(const LinearA
         for (int i = j * kWPer; i < (j + 1) * kWPer; ++i)
           if (i < FN) read_w(next, 0, i);
         read_x(next, 0, j);
-#pragma unroll
-        for (int l = j * kLoadsPer; l < (j + 1) * kLoadsPer; ++l)
-          if (l < kLoads) load(l, buffer);
+        load_some(j, buffer);
       });
       read_x(next, 0, kHalf + j);
     }
+    const int read_out = buffer;
     buffer = next;
-    first_step(buffer);
+    first_step(buffer, read_out);
 #pragma unroll
     for (int j = 0; j < kHalf; ++j) group(1, j, [] {});
   }
 #pragma unroll
-  for (int j = FM / 2; j < FM; ++j) group(1, j, [] {});
+  for (int j = kHalf; j < FM; ++j) group(1, j, [] {});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing arrives in LDS that is another workgroup's by then
 
   if (threadIdx.x < BM) x_scales[threadIdx.x] = row_scale;
@@ -408,8 +416,8 @@ template <typename T, int MT, int NT, int DEPTH, int WAVES> int launch_rows(cons
 }
 
 // Which blocks: those whose rounds over the compute units take least.  us for 40 stages of 128 channels and so many blocks, on 256 compute units:
-//   256 x 256   68 for each round of 256                                      (256 blocks 68, 480 145)
-//   128 x 128   42 for up to 256, then 46 for each round of 512               (240: 42, 480: 50, 960: 91, 1,920: 175)
+//   256 x 256   65 for each round of 256                                      (256 blocks 65, 480 142)
+//   128 x 128   40 for up to 256, then 46 for each round of 512               (240: 39, 480: 47, 960: 88, 1,920: 167)
 //    64 x 64    19 for up to 256, then 10 and 0.036 a block                   (320: 28, 960: 47, 2,560: 104)
 //    32 x 32, wavefronts apart   8 and 0.015 a block                          (160: 10.7, 640: 18, 1,280: 27, 2,560: 45)
 // and up to 16 rows: 16 x 32 with 8 wavefronts (5,120 channels and outputs, weights from memory: 8.2 - 9.4; 16 x 16 with 4 8.8 - 10.4, 32 x 32 8.7 - 9.6), or
@@ -419,7 +427,7 @@ template <typename T> int launch_best(LinearArgs& a, const LinearTable& tab, hip
   auto blocks = [&](int64_t bm, int64_t bn) { return ((rows + bm - 1) / bm) * ((outputs + bn - 1) / bn); };
   if (rows <= 16) return blocks(16, 32) >= 64 ? launch_rows<T, 1, 2, 3, 8>(a, tab, s) : launch_rows<T, 1, 1, 4, 4>(a, tab, s);
   const int64_t b256 = blocks(256, 256), b128 = blocks(128, 128), b64 = blocks(64, 64), b32 = blocks(32, 32);
-  const int64_t t256 = (b256 + 255) / 256 * 68000, t128 = b128 <= 256 ? 42000 : (b128 + 511) / 512 * 46000, t64 = b64 <= 256 ? 19000 : 10000 + 36 * b64,
+  const int64_t t256 = (b256 + 255) / 256 * 65000, t128 = b128 <= 256 ? 40000 : (b128 + 511) / 512 * 46000, t64 = b64 <= 256 ? 19000 : 10000 + 36 * b64,
                 t32 = 8000 + 15 * b32;
   // (a grid has less than 2^32 threads: 256 of a workgroup, 512 of the largest blocks, whose number the call's checks bound)
   constexpr int64_t kMost = (1ll << 24) - 1;
