@@ -5,9 +5,11 @@
 // passes over the heads, each lane with 16 channels of one head as two vectors of 8 whose pairs lie in the lane.  The angle is a product in fp64
 // (positions reach millions of turns), reduced to a part of one turn there, and only that is rounded to fp32.
 //
-// Bound by memory, every channel read and written once: 75,600 tokens of 40 + 40 heads x 128 in bf16, token-major 570 us (5.4 TB/s; a large copy runs at 4.9), with
-// the norm of the heads 585, head-major 625 - 640; 9 x 4,000 tokens of 40 + 8 heads 172 us (5.1).  Few short heads are bound by the sines: 9 tiles of 75,600
-// tokens, 1 + 1 heads x 64 100 us (3.5 TB/s).
+// Bound by memory, every channel read and written once: 75,600 tokens of 40 + 40 heads x 128 in bf16, token-major, with or without the norm of the heads 537 us
+// (5.8 TB/s; a large copy runs at 5.0), head-major 602; 9 x 4,000 tokens of 40 + 8 heads 162 us (5.5).  The arithmetic has to stay below it: with factors and
+// places found anew for every head and each pair asked whether it turns, the vector units were 96 % busy and the first of these took 587 us.  So q and k are
+// passes of their own with their weight in registers, offsets are 32 bits where they fit, and heads that turn whole have a form without questions.  Few short heads
+// are bound by the sines: 9 tiles of 75,600 tokens, 1 + 1 heads x 64 97 us (3.6 TB/s).
 #include "block_api.h"
 #include "row_common.h"
 
@@ -36,14 +38,16 @@ struct RotaryArgs {
   int32_t turned, first_y, first_x;             // channels that turn; first pair of the axes y and x
   int32_t H_W, W, position_axes;
   int32_t canvas[3];
-  Divisor by_plane, by_row, by_chunks, by_heads;
+  Divisor by_plane, by_row, by_chunks, by_heads, by_kv_heads;
+  bool near;                                    // offsets inside a workgroup's tokens are below 2^32 elements
   bool by_token;                                // rows in the order of memory: heads of a token side by side
-  float eps;
+  float eps, by_channels;
 };
 
-template <typename T, bool HALF, bool LINES>
+// HALF: layout; LINES: a load of a head's lanes takes whole cache lines; FULL: every channel turns and every lane has two vectors
+template <typename T, bool HALF, bool LINES, bool FULL>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const RotaryTable tab) {
-  extern __shared__ float turns[];   // [chunk][pairs padded to 8] cosines, then sines
+  extern __shared__ __align__(16) float turns[];   // [chunk][pairs padded to 8] cosines, then sines
   const int tile = (int)divide(blockIdx.x, a.by_chunks);
   if (a.run && a.run[tile] == 0) return;
   const int token0 = (int)(blockIdx.x - (uint32_t)tile * (uint32_t)a.chunks) << a.chunk_shift;
@@ -52,41 +56,42 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const R
   float* const cosines = turns;
   float* const sines = turns + a.chunk * row_pairs;
 
-  const int head0 = blockIdx.y * a.head_step;
-  const int n_heads = a.all_heads - head0 < a.head_step ? a.all_heads - head0 : a.head_step;
-  const int n_rows = n_heads * n_tokens;
   const int l = threadIdx.x & (a.lanes - 1);
   // The lane's vectors: HALF: those of the channels that turn meet their partners, half of them behind; the others two by two.
   const int half = a.turned >> 4;
-  const bool has_a = 2 * l < a.n_vec || (!HALF && l < (a.n_vec + 1) / 2);
+  const bool has_a = FULL || 2 * l < a.n_vec || (!HALF && l < (a.n_vec + 1) / 2);
   int va, vb;
   if (HALF) {
-    va = l < half ? l : 2 * l;
-    vb = l < half ? l + half : 2 * l + 1;
+    va = FULL || l < half ? l : 2 * l;
+    vb = FULL || l < half ? l + half : 2 * l + 1;
   } else {
     va = l;
     vb = l + (a.n_vec + 1) / 2;
   }
-  const bool has_b = has_a && vb < a.n_vec;
+  const bool has_b = FULL || (has_a && vb < a.n_vec);
+
+  // The workgroup's heads: of q, then of k.
+  const int step = 256 >> a.lane_shift;
+  const int head0 = blockIdx.y * a.head_step, head1 = min(head0 + a.head_step, a.all_heads);
+  const int q_heads = max(min(head1, a.heads) - head0, 0), k_heads = head1 - max(head0, a.heads);
+  // Its row r of n heads as (token, head).
   struct Row { int t, head; };
-  auto row_of = [&](int r) {
+  auto row_of = [&](int r, int n) {
     int t, head;
     if (a.by_token) {
-      t = n_heads == a.all_heads ? (int)divide((uint32_t)r, a.by_heads) : r / n_heads;
-      head = r - t * n_heads;
+      t = n == a.heads ? (int)divide((uint32_t)r, a.by_heads) : n == a.all_heads - a.heads ? (int)divide((uint32_t)r, a.by_kv_heads) : r / n;
+      head = r - t * n;
     } else {
       head = n_tokens == a.chunk ? r >> a.chunk_shift : r / n_tokens;
       t = r - head * n_tokens;
     }
-    return Row{t, head + head0};
+    return Row{t, head};
   };
-  const T* const q = (const T*)tab.q[tile] + token0 * a.q_token;
-  const T* const k = (const T*)tab.k[tile] + token0 * a.k_token;   // (from here on offsets of the workgroup's tokens)
-  T* const q_out = (T*)tab.q_out[tile] + token0 * a.qo_token;
-  T* const k_out = (T*)tab.k_out[tile] + token0 * a.ko_token;
+  auto offset = [&](Row w, int64_t token, int64_t head) -> int64_t {
+    return a.near ? (int64_t)((uint32_t)w.t * (uint32_t)token + (uint32_t)w.head * (uint32_t)head) : w.t * token + w.head * head;
+  };
   Chan8<T> ra, rb;
-  auto fetch = [&](Row w) {
-    const T* const x = w.head >= a.heads ? k + w.t * a.k_token + (w.head - a.heads) * a.k_head : q + w.t * a.q_token + w.head * a.q_head;
+  auto fetch = [&](const T* x) {
     if constexpr (LINES) {
       if (has_a) ra.stream(x + 8 * va);
       if (has_b) rb.stream(x + 8 * vb);
@@ -96,10 +101,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const R
     }
   };
   // The first rows are on their way while the sines are computed, the next ones while a row is turned.
-  const int step = 256 >> a.lane_shift;
-  int r = threadIdx.x >> a.lane_shift;
-  Row now = row_of(r < n_rows ? r : 0);
-  if (r < n_rows) fetch(now);
+  const T* const q = (const T*)tab.q[tile] + token0 * a.q_token + head0 * a.q_head;
+  if (q_heads > 0 && (int)(threadIdx.x >> a.lane_shift) < q_heads * n_tokens) fetch(q + offset(row_of(threadIdx.x >> a.lane_shift, q_heads), a.q_token, a.q_head));
 
   for (int i = threadIdx.x; i < n_tokens * row_pairs; i += 256) {
     const int t = i / row_pairs, pair = i - t * row_pairs;
@@ -131,81 +134,100 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a, const R
   }
   __syncthreads();
 
-  for (; r < n_rows;) {
-    float u[8], v[8];
+  auto turn_heads = [&](const T* const x, T* const y, int heads, int64_t x_token, int64_t x_head, int64_t y_token, int64_t y_head, const T* const weight, bool fetched) {
+    const int n_rows = heads * n_tokens;
+    int r = threadIdx.x >> a.lane_shift;
+    if (r >= n_rows) return;
+    Row now = row_of(r, heads);
+    if (!fetched) fetch(x + offset(now, x_token, x_head));
+    Chan8<T> wa, wb;
+    wa.clear();
+    wb.clear();
+    if (weight && has_a) wa.load(weight + 8 * va);
+    if (weight && has_b) wb.load(weight + 8 * vb);
+    for (; r < n_rows;) {
+      float u[8], v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      u[e] = has_a ? ra.get(e) : 0.f;
-      v[e] = has_b ? rb.get(e) : 0.f;
-    }
-    const int t = now.t;
-    const bool is_k = now.head >= a.heads;
-    const T* const weight = (const T*)(is_k ? a.k_weight : a.q_weight);
-    T* const y = is_k ? k_out + t * a.ko_token + (now.head - a.heads) * a.ko_head : q_out + t * a.qo_token + now.head * a.qo_head;
-    r += step;
-    if (r < n_rows) {
-      now = row_of(r);
-      fetch(now);
-    }
-    if (a.q_weight || a.k_weight) {   // (the lanes of a row agree on `weight`)
-      float sq = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sq += u[e] * u[e] + v[e] * v[e];
-      const float mean = sum_over_lanes(sq, a.lanes) / (float)a.channels + a.eps;
-      float norm = rsqrtf(mean), by = 1.f;
-      const bool odd = !(mean >= kLeastMean && mean <= kMostFloat);
-      if (__any(odd)) {
-        const float to = mean < kLeastMean ? kGrowRow : kShrinkRow;
-        sq = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sq += (u[e] * to) * (u[e] * to) + (v[e] * to) * (v[e] * to);
-        const float other = rsqrtf(sum_over_lanes(sq, a.lanes) / (float)a.channels + a.eps * to * to);
-        if (odd) { norm = other; by = to; }
+      for (int e = 0; e < 8; ++e) {
+        u[e] = has_a ? ra.get(e) : 0.f;
+        v[e] = has_b ? rb.get(e) : 0.f;
+      }
+      const int t = now.t;
+      T* const to = y + offset(now, y_token, y_head);
+      r += step;
+      if (r < n_rows) {
+        now = row_of(r, heads);
+        fetch(x + offset(now, x_token, x_head));
       }
       if (weight) {
-        Chan8<T> wa, wb;
-        if (has_a) wa.load(weight + 8 * va);
-        if (has_b) wb.load(weight + 8 * vb);
+        float sq = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq = fmaf(u[e], u[e], fmaf(v[e], v[e], sq));
+        const float mean = sum_over_lanes(sq, a.lanes) * a.by_channels + a.eps;
+        float norm = rsqrtf(mean);
+        const bool odd = !(mean >= kLeastMean && mean <= kMostFloat);
+        if (__any(odd)) {
+          const float to_range = !odd ? 1.f : mean < kLeastMean ? kGrowRow : kShrinkRow;
+          sq = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            u[e] *= to_range;
+            v[e] *= to_range;
+            sq = fmaf(u[e], u[e], fmaf(v[e], v[e], sq));
+          }
+          const float other = rsqrtf(sum_over_lanes(sq, a.lanes) * a.by_channels + a.eps * to_range * to_range);
+          if (odd) norm = other;
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          if (has_a) u[e] = u[e] * by * norm * wa.get(e);
-          if (has_b) v[e] = v[e] * by * norm * wb.get(e);
+          u[e] = u[e] * norm * wa.get(e);
+          v[e] = v[e] * norm * wb.get(e);
         }
       }
-    }
-    const float* const c = cosines + t * row_pairs;
-    const float* const s = sines + t * row_pairs;
-    if (HALF) {
-      if (l < half) {
+      const float* const c = cosines + t * row_pairs;
+      const float* const s = sines + t * row_pairs;
+      if (HALF) {
+        if (FULL || l < half) {
+          Chan8<float> cs, sn;
+          cs.load(c + 8 * l);
+          sn.load(s + 8 * l);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float cs = c[8 * l + e], sn = s[8 * l + e], p = u[e], q = v[e];
-          u[e] = p * cs - q * sn;
-          v[e] = q * cs + p * sn;
+          for (int e = 0; e < 8; ++e) {
+            const float p = u[e], q = v[e];
+            u[e] = p * cs.get(e) - q * sn.get(e);
+            v[e] = q * cs.get(e) + p * sn.get(e);
+          }
         }
-      }
-    } else {
+      } else {
+        auto turn4 = [&](float (&w)[8], int first) {   // pairs first .. first + 3
+          if (!FULL && first >= row_pairs) return;
+          const f32x4 cs = *(const f32x4*)(c + first), sn = *(const f32x4*)(s + first);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (4 * va + e < pairs) {
-          const float cs = c[4 * va + e], sn = s[4 * va + e], p = u[2 * e], q = u[2 * e + 1];
-          u[2 * e] = p * cs - q * sn;
-          u[2 * e + 1] = q * cs + p * sn;
-        }
-        if (4 * vb + e < pairs) {
-          const float cs = c[4 * vb + e], sn = s[4 * vb + e], p = v[2 * e], q = v[2 * e + 1];
-          v[2 * e] = p * cs - q * sn;
-          v[2 * e + 1] = q * cs + p * sn;
-        }
+          for (int e = 0; e < 4; ++e)
+            if (FULL || first + e < pairs) {
+              const float p = w[2 * e], q = w[2 * e + 1];
+              w[2 * e] = p * cs[e] - q * sn[e];
+              w[2 * e + 1] = q * cs[e] + p * sn[e];
+            }
+        };
+        turn4(u, 4 * va);
+        turn4(v, 4 * vb);
+      }
+      if constexpr (LINES) {
+        if (has_a) stream8(to + 8 * va, u);
+        if (has_b) stream8(to + 8 * vb, v);
+      } else {
+        if (has_a) store8(to + 8 * va, u);
+        if (has_b) store8(to + 8 * vb, v);
       }
     }
-    if constexpr (LINES) {
-      if (has_a) stream8(y + 8 * va, u);
-      if (has_b) stream8(y + 8 * vb, v);
-    } else {
-      if (has_a) store8(y + 8 * va, u);
-      if (has_b) store8(y + 8 * vb, v);
-    }
+  };
+  if (q_heads > 0)
+    turn_heads(q, (T*)tab.q_out[tile] + token0 * a.qo_token + head0 * a.qo_head, q_heads, a.q_token, a.q_head, a.qo_token, a.qo_head, (const T*)a.q_weight, true);
+  if (k_heads > 0) {
+    const int first = max(head0, a.heads) - a.heads;
+    turn_heads((const T*)tab.k[tile] + token0 * a.k_token + first * a.k_head, (T*)tab.k_out[tile] + token0 * a.ko_token + first * a.ko_head, k_heads, a.k_token, a.k_head,
+               a.ko_token, a.ko_head, (const T*)a.k_weight, false);
   }
 }
 
@@ -228,11 +250,13 @@ int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q,
   a.H_W = p.H * p.W; a.W = p.W; a.position_axes = p.position_axes;
   a.canvas[0] = p.canvas_t; a.canvas[1] = p.canvas_h; a.canvas[2] = p.canvas_w;
   a.by_plane = make_divisor((uint32_t)a.H_W); a.by_row = make_divisor((uint32_t)p.W);
-  a.by_heads = make_divisor((uint32_t)a.all_heads);
+  a.by_heads = make_divisor((uint32_t)a.heads);
+  a.by_kv_heads = make_divisor((uint32_t)(k ? p.kv_heads : 1));
   a.by_token = p.q_stride_head < p.q_stride_token;
   a.eps = p.eps;
+  a.by_channels = 1.f / (float)p.head_dim;
   // Tokens of a workgroup: rows for one pass of it at least and 8 at most, where that leaves 2,048 workgroups (2 x 36 x 40 tokens, 4 tiles, 8 + 8 heads of 128,
-  // fp32: 45 us, with 8 passes 49); heads that lie apart: for runs of 4 KiB, up to 64 passes (75,600 tokens 640 us, with 8 662).  Its table within 32 KiB.
+  // fp32: 45 us, with 8 passes 49); heads that lie apart: for runs of 4 KiB, up to 64 passes (75,600 tokens 602 us, with 8 630).  Its table within 32 KiB.
   const int rows_per_pass = 256 >> a.lane_shift, row_pairs = (a.turned / 2 + 7) & ~7;
   const int passes_most = a.by_token ? 8 : 64;
   const int run_bytes = p.head_dim * (p.dtype == SG_F32 ? 4 : 2);
@@ -245,6 +269,11 @@ int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q,
   a.chunks = (a.tokens + a.chunk - 1) / a.chunk;
   a.by_chunks = make_divisor((uint32_t)a.chunks);
   const size_t lds = (size_t)a.chunk * row_pairs * 8;
+  auto reach = [&](int64_t token, int64_t head, int64_t heads) {   // (in doubles: the products can pass 64 bits)
+    return (double)(a.chunk - 1) * (double)token + (double)(heads - 1) * (double)head < 4294967296.0 && token < (1ll << 32) && head < (1ll << 32);
+  };
+  a.near = reach(a.q_token, a.q_head, a.heads) && reach(a.qo_token, a.qo_head, a.heads) &&
+           (!k || (reach(a.k_token, a.k_head, p.kv_heads) && reach(a.ko_token, a.ko_head, p.kv_heads)));
   // A grid has less than 2^32 threads: 2^24 workgroups, times the parts of few tokens' heads.
   int most_tiles = ((1 << 24) - 1) / a.chunks;
   most_tiles = most_tiles < 1 ? 1 : most_tiles > kRotaryTilesPerLaunch ? kRotaryTilesPerLaunch : most_tiles;
@@ -273,19 +302,25 @@ int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q,
     splits = (a.all_heads + a.head_step - 1) / a.head_step;
     const dim3 grid((unsigned)wgs, (unsigned)splits);
     // Where a load of a head's lanes takes whole cache lines, they pass the caches by; other heads' lines are met twice (4 tiles of 75,600 tokens, 5 + 5 heads
-    // x 96 309 us, past the caches 356).
-    const bool half = p.layout == SG_ROTARY_HALF, lines = p.head_dim % 128 == 0;
-#define SG_ROTARY(T, H, L) rotary_kernel<T, H, L><<<grid, 256, lds, s>>>(a, tab)
+    // x 96: past the caches a seventh more).
+    const bool half = p.layout == SG_ROTARY_HALF, lines = p.head_dim % 128 == 0, full = a.turned == p.head_dim && a.n_vec == 2 * a.lanes;
+#define SG_ROTARY(T, H, L, F) rotary_kernel<T, H, L, F><<<grid, 256, lds, s>>>(a, tab)
+#define SG_ROTARY_FULL(T, H, L)             \
+  do {                                      \
+    if (full) SG_ROTARY(T, H, L, true);     \
+    else SG_ROTARY(T, H, L, false);         \
+  } while (0)
     if (p.dtype == SG_F32) {
-      if (half) SG_ROTARY(float, true, false);
-      else SG_ROTARY(float, false, false);
+      if (half) SG_ROTARY_FULL(float, true, false);
+      else SG_ROTARY_FULL(float, false, false);
     } else if (lines) {
-      if (half) SG_ROTARY(uint16_t, true, true);
-      else SG_ROTARY(uint16_t, false, true);
+      if (half) SG_ROTARY_FULL(uint16_t, true, true);
+      else SG_ROTARY_FULL(uint16_t, false, true);
     } else {
-      if (half) SG_ROTARY(uint16_t, true, false);
-      else SG_ROTARY(uint16_t, false, false);
+      if (half) SG_ROTARY_FULL(uint16_t, true, false);
+      else SG_ROTARY_FULL(uint16_t, false, false);
     }
+#undef SG_ROTARY_FULL
 #undef SG_ROTARY
     SG_HIP_TRY(hipGetLastError());
   }
