@@ -5,8 +5,8 @@
 // passes over the heads, each lane with 16 channels of one head as two vectors of 8 whose pairs lie in the lane.  The angle is a product in fp64
 // (positions reach millions of turns), reduced to a part of one turn there, and only that is rounded to fp32.
 //
-// Bound by memory, every channel read and written once: 75,600 tokens of 40 + 40 heads x 128 in bf16, token-major, with or without the norm of the heads 537 us
-// (5.8 TB/s; a large copy runs at 5.0), head-major 602; 9 x 4,000 tokens of 40 + 8 heads 162 us (5.5).  The arithmetic has to stay below it: with factors and
+// Bound by memory, every channel read and written once: 75,600 tokens of 40 + 40 heads x 128 in bf16, token-major, with or without the norm of the heads 510 us
+// (6.1 TB/s; a large copy runs at 5.0), head-major 605; 9 x 4,000 tokens of 40 + 8 heads 153 us (5.8).  The arithmetic has to stay below it: with factors and
 // places found anew for every head and each pair asked whether it turns, the vector units were 96 % busy and the first of these took 587 us.  So q and k are
 // passes of their own with their weight in registers, offsets are 32 bits where they fit, and heads that turn whole have a form without questions.  Few short heads
 // are bound by the sines: 9 tiles of 75,600 tokens, 1 + 1 heads x 64 97 us (3.6 TB/s).
@@ -255,10 +255,11 @@ int launch_rotary(const sg_rotary_problem& p, int n_tiles, const void* const* q,
   a.by_token = p.q_stride_head < p.q_stride_token;
   a.eps = p.eps;
   a.by_channels = 1.f / (float)p.head_dim;
-  // Tokens of a workgroup: rows for one pass of it at least and 8 at most, where that leaves 2,048 workgroups (2 x 36 x 40 tokens, 4 tiles, 8 + 8 heads of 128,
-  // fp32: 45 us, with 8 passes 49); heads that lie apart: for runs of 4 KiB, up to 64 passes (75,600 tokens 602 us, with 8 630).  Its table within 32 KiB.
+  // Tokens of a workgroup: rows for one pass of it at least, where that leaves 2,048 workgroups (2 x 36 x 40 tokens, 4 tiles, 8 + 8 heads of 128, fp32: 45 us, with 8
+  // passes 49), and for few passes: 4 over heads of whole cache lines that lie side by side (75,600 tokens, 40 + 40 heads x 128 509 us; 2 523, 8 543, 16 569), 8 over
+  // others (4 tiles, 5 + 5 heads x 96 244; 4 274).  Heads that lie apart: for runs of 4 KiB, up to 64 passes (605 us; 8 626, 2 677).  Its table within 32 KiB.
   const int rows_per_pass = 256 >> a.lane_shift, row_pairs = (a.turned / 2 + 7) & ~7;
-  const int passes_most = a.by_token ? 8 : 64;
+  const int passes_most = !a.by_token ? 64 : p.head_dim % 128 == 0 ? 4 : 8;
   const int run_bytes = p.head_dim * (p.dtype == SG_F32 ? 4 : 2);
   a.chunk = 1; a.chunk_shift = 0;
   while (a.chunk < 64 && a.chunk < a.tokens && 2 * a.chunk * row_pairs * 8 <= 32768) {
