@@ -4,7 +4,7 @@
 // residual, one write of s and out.  Bound by memory.
 //
 // 75,600 rows of 5,120, bf16, layer norm with gate, scale and shift to e4m3 483 us (5.6 TB/s; a large copy runs at 4.9), with those in fp32 613; 4 tiles of
-// 2,925 rows of 1,536 with a norm of x and fp32 vectors for each 225 rows 34 us (4.2); 10^6 rows of 128 205 us (5.0).
+// 2,925 rows of 1,536 with a norm of x and fp32 vectors for each 225 rows 34 us (4.2); 10^6 rows of 128 186 us (5.5).
 //
 // What keeps it from the memory's rate is the arithmetic beside it (some 550 vector instructions for 24 channels of a wavefront, half of the time) and the
 // chain of latencies of a row: loads, one or two reductions, loads of what the reductions stand in front of, stores.  So a lane holds 3 vectors of 8
@@ -205,9 +205,21 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
     const bool there = LONG || runs;
     const int64_t vec = (int64_t)divide((uint32_t)row, a.by_mod) * a.m_stride;
     const T* const x = (const T*)tab.x[tile] + row * a.x_stride;
+    constexpr bool kInRegisters = !LONG;
     Chan8<M> near[3][VPL];   // short rows: in registers
+    auto ask = [&](int what, const void* from, bool has) {
+      if constexpr (kInRegisters) {
+        if (has) {
+#pragma unroll
+          for (int i = 0; i < VPL; ++i) {
+            near[what][i].clear();
+            if (there && on(i)) near[what][i].load((const M*)from + vec + 8 * (first + i * lanes));
+          }
+        }
+      }
+    };
     auto vector_of = [&](int what, int i, const void* from) {
-      if constexpr (!LONG) return near[what][i];
+      if constexpr (kInRegisters) return near[what][i];
       if (what < a.early) return kept(what, i);
       Chan8<M> v;
       v.clear();
@@ -216,18 +228,8 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
     };
     // Everything that the row needs is asked for at once.  Gate, scale and shift of long rows wait in LDS, each lane's in its own place, which takes no
     // registers and no barrier.
-    if constexpr (!LONG) {
-#pragma unroll
-      for (int i = 0; i < VPL; ++i) {
-        const int c = 8 * (first + i * lanes);
-#pragma unroll
-        for (int what = 0; what < 3; ++what) near[what][i].clear();
-        if (there && on(i)) {
-          if (a.has_gate) near[0][i].load((const M*)tab.gate[tile] + vec + c);
-          if (a.has_scale) near[1][i].load((const M*)tab.scale[tile] + vec + c);
-          if (a.has_shift) near[2][i].load((const M*)tab.shift[tile] + vec + c);
-        }
-      }
+    if constexpr (kInRegisters) {
+      ask(0, tab.gate[tile], a.has_gate);
     } else {
 #pragma unroll
       for (int i = 0; i < VPL; ++i)
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
         if (there && on(i)) rv[i].stream(r + 8 * (first + i * lanes));
       }
     }
-    if (LONG) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (!kInRegisters) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int i = 0; i < VPL; ++i)
 #pragma unroll
@@ -293,6 +295,8 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
       for (int i = 0; i < VPL; ++i)
         if (there && on(i)) stream8(o + 8 * (first + i * lanes), s[i]);
     }
+    ask(1, tab.scale[tile], a.has_scale);
+    ask(2, tab.shift[tile], a.has_shift);
     normalise(s, a.norm, a.eps);
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
@@ -419,7 +423,7 @@ int launch_gated_norm(const sg_gated_norm_problem& p, int n_tiles, const void* c
   a.has_sum = sum != nullptr;
   a.residual_scale = p.residual_scale; a.eps = p.eps; a.post_eps = p.post_eps;
   a.by_channels = 1.f / (float)p.channels;
-  // Up to 256 channels rows share a wavefront, 2 vectors a lane (10^6 rows of 128 channels 205 us, one vector 343; with blocks of 128 channels always one,
+  // Up to 256 channels rows share a wavefront, 2 vectors a lane (10^6 rows of 128 channels 186 us, one vector 343 in an earlier form; with blocks of 128 channels always one,
   // which leaves a block to 16 lanes side by side).  512 channels: one wavefront with one vector a lane (400,000 rows 270 us; shared 313).  Then up to 3
   // vectors; beyond 6,144 channels 2 (30,000 rows of 8,192 340 us; 3: 450) up to 16 wavefronts and beyond 16,384 4.
   const bool is_short = a.n_vec <= 32;
@@ -457,7 +461,7 @@ int launch_gated_norm(const sg_gated_norm_problem& p, int n_tiles, const void* c
     a.n_rows = (uint32_t)n * (uint32_t)p.rows;
     a.run = run ? run + t0 : nullptr;
     uint32_t grid = (a.n_rows + rows_per_wg - 1) / rows_per_wg;
-    // New workgroups for new rows: walking them, 2,048 workgroups take 344 us instead of 205 for 10^6 rows of 128 channels.  (2^21 a launch, then they walk.)
+    // New workgroups for new rows: walking them, 2,048 workgroups took 344 us instead of 205 for 10^6 rows of 128 channels.  (2^21 a launch, then they walk.)
     if (grid > 1u << 21) grid = 1u << 21;
     const int st = p.dtype == SG_F32      ? launch<float, float>(a, tab, is_short, vpl, threads, grid, s)
                    : p.mod_dtype == SG_F32 ? launch<uint16_t, float>(a, tab, is_short, vpl, threads, grid, s)
