@@ -65,7 +65,7 @@ template <typename T> __device__ __forceinline__ void finish8(const LinearArgs& 
   store8(out, v);
 }
 
-// The tiles of a launch that run, in their order; false if there are none.  list: LDS.  (All threads of the workgroup.)
+// The tiles of a launch that run, in their order, into list (LDS); how many.  (All threads of the workgroup.)
 __device__ __forceinline__ int running_tiles(const LinearArgs& a, int* list) {
   const int lane = threadIdx.x & 63;
   const bool runs = lane < a.n_tiles && (!a.run || a.run[lane] != 0);
