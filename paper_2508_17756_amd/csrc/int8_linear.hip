@@ -7,10 +7,10 @@
 // w is the instruction's first operand, its rows in an order that leaves a lane with outputs side by side of one row, which it scales and stores together.
 //
 // Large calls: held in registers, N(0, 32)-distributed integers pass the instruction at 3.9 POP/s, bound by power (zeros: 4.9; the form 32x32x32, which touches each
-// sum twice as often, at 3.3).  Blocks of 256 x 256: 34,560 x 5,120 x 15,360 2.19 ms = 2.48 POP/s, 75,600 x 5,120 x 20,480 with GELU 6.7 - 6.8 ms = 2.33 - 2.37.  A
-// block's 40 stages take seven eighths of its time, the matrix pipe busy for 0.7 of them: what is lost there is the barrier of each stage, where the two
-// wavefronts of a SIMD leave it empty, and in the last eighth its start and its stores.  32x32x32 instead: 2.58 ms at the first size; all of a stage's loads
-// behind its barrier: 2.23; factors and places of the rows looked up at the end: 2.35.
+// sum twice as often, at 3.3).  Blocks of 256 x 256: 34,560 x 5,120 x 15,360 2.15 - 2.19 ms = 2.48 - 2.53 POP/s (all zeros: 1.74 ms), 75,600 x 5,120 x 20,480 with GELU
+// 6.6 - 6.8 ms.  A block's 40 stages take seven eighths of its time, its start and its stores the last.  What the stages lose, timed with parts left out, are
+// the loads from the L2 into LDS (64 KiB a stage; without them 1.76 ms, zeros 1.43), hardly the barriers (a further 0.02) and not the reads of LDS.
+// 32x32x32 instead: 2.58 ms at the first size; all of a stage's loads behind its barrier: 2.23; factors and places of the rows looked up at the end: 2.35.
 #include <atomic>
 #include "block_api.h"
 #include "row_common.h"
