@@ -634,8 +634,10 @@ typedef struct sg_gated_norm_problem {
  *                where one of its y is NaN or infinite the scale is NaN (and so is what the 8 bits stand for).  Aliases nothing
  *   out_scale    8 bits: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats; else NULL
  *   run          device, n_tiles bytes, or NULL: all tiles
- * Everything is fp32 between the loads and the stores: y comes from the sum before it is rounded, for every finite s, as in sg_tile_residual_norm; the
- * mean of SG_NORM_LAYER is taken twice, the second time of what the first leaves, so that rows far from 0 keep their digits.  With eps = 0 a row of zeros
+ * Everything is fp32 between the loads and the stores: y comes from the sum before it is rounded, for every finite s, as in sg_tile_residual_norm.  Mean
+ * and variance of SG_NORM_LAYER come from one pass, mean(v^2) - mean(v)^2, where mean^2 <= variance / 4 (which loses less than two bits); of rows farther
+ * from 0 the mean is taken again of what it leaves, so that they keep their digits, and of rows of nearly one value once more.  A row of one value gives
+ * 0, however large it is (below 2^-50 in size: up to 2^-18 of it / sqrt(eps)).  With eps = 0 a row of zeros
  * (SG_NORM_LAYER: of one value) gives NaN.  A row with a NaN is NaN throughout, and so is one with an infinity behind SG_NORM_LAYER (SG_NORM_RMS: NaN there, 0
  * elsewhere).  All pointers 16-byte aligned (out_scale: 4).
  */

@@ -97,6 +97,10 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
   // v <- norm(v).  Places behind the row's end hold 0 before and anything afterwards.
   // mean and variance come from one pass, mean(v^2) - mean(v)^2, where that loses less than two bits, mean^2 <= variance / 4; rows farther from 0
   // take a second pass: with m1 = mean(v), d = v - m1, m2 = mean(d), which is what rounding left in m1: variance = mean(d^2) - m2^2, v - mean = d - m2.
+  // Where rounding left more than half a deviation (rows of one value, or nearly one, whatever its size) nothing is left of that difference either, and
+  // where a sum left fp32 there is none: a third pass takes the mean once more, of what the second leaves or of the row brought into range by a power of
+  // two, and puts it between the least and the largest of those numbers, which no mean leaves: a row of one value has no deviations then, and in others they
+  // are never larger than the row is wide.
   auto normalise = [&](float (&v)[VPL][8], int kind, float eps) {
     float m1 = 0.f, m2 = 0.f, sq = 0.f;
     const bool layer = kind == SG_NORM_LAYER;
@@ -121,8 +125,9 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
     const bool again = !(mean >= kLeastMean && mean <= kMostFloat && m1 * m1 <= 0.25f * sq);
     if (LONG ? again : __any(again)) {
       const float m0 = m1;
-      float q = 0.f;
+      bool off = false;
       if (layer) {
+        float q = 0.f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i)
           if (on(i)) {
@@ -132,24 +137,33 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
         row_sums(m2, q);
         m2 *= by_channels;
         q = q * by_channels - m2 * m2;
-        if (q < 0.f) q = 0.f;   // (a NaN stays)
+        off = !(m2 * m2 <= 0.25f * q);
         mean = q + eps;
       }
-      const bool odd = !(mean >= kLeastMean && mean <= kMostFloat);
-      const bool grow = mean < kLeastMean;
-      const float to = odd ? grow ? kGrowRow : kShrinkRow : 1.f;
-      // s brings the row into the range: what is too small once its mean is gone, what is too large before it is taken
-      auto at = [&](int i, int e) { return grow || !odd ? (v[i][e] - m0 - m2) * to : v[i][e] * to; };
+      const bool odd = !(mean >= kLeastMean && mean <= kMostFloat), third = odd || off;
+      const bool late = !odd || mean < kLeastMean;
+      const float to = !odd ? 1.f : late ? kGrowRow : kShrinkRow;
+      // `to` brings the row into the range: what is too small once its mean is gone, what is too large before it is taken
+      auto at = [&](int i, int e) { return late ? (v[i][e] - m0 - m2) * to : v[i][e] * to; };
       float n1 = 0.f, n2 = 0.f;
-      if (LONG ? odd : __any(odd)) {
+      if (LONG ? third : __any(third)) {
         if (layer) {
+          float least = __builtin_inff(), most = -__builtin_inff();
 #pragma unroll
           for (int i = 0; i < VPL; ++i)
             if (on(i)) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) n1 += at(i, e);
+              for (int e = 0; e < 8; ++e) {
+                const float u = at(i, e);
+                n1 += u;
+                least = __builtin_elementwise_minimum(least, u);
+                most = larger_or_nan(most, u);
+              }
             }
           n1 = row_sum(n1) * by_channels;
+          least = -row_max(-least);
+          most = row_max(most);
+          n1 = __builtin_elementwise_minimum(larger_or_nan(n1, least), most);
         }
         float w = 0.f;
 #pragma unroll
@@ -161,9 +175,13 @@ __global__ __launch_bounds__(LONG && VPL != 3 ? 1024 : 256, LONG && VPL == 3 && 
         row_sums(n2, w);
         n2 = layer ? n2 * by_channels : 0.f;
         w = w * by_channels - n2 * n2;
-        if (w < 0.f) w = 0.f;
-        if (odd) mean = w + eps * to * to;
-        else n1 = n2 = 0.f;
+        if (w < 0.f) w = 0.f;   // (a NaN stays)
+        if (third) {
+          mean = w + eps * to * to;
+          if (mean == 0.f && eps > 0.f) mean = 1.f;   // no deviations; eps 2^-144 has left fp32, but it is there
+        } else {
+          n1 = n2 = 0.f;
+        }
       }
       const float other = rsqrtf(mean);
 #pragma unroll
