@@ -632,7 +632,7 @@ typedef struct sg_gated_norm_problem {
  *   out          host array: y in the tensors' type; or in 8 bits, y * (M / max|y|) rounded to the nearest (ties to even), out_scale = max|y| / M, with
  *                M = 448 (SG_F8_E4M3) or 127 (SG_I8), the maximum over a row or over each 128 channels of it; below 2^-100: zeros and a scale of 0;
  *                where one of its y is NaN or infinite the scale is NaN (and so is what the 8 bits stand for).  Aliases nothing
- *   out_scale    8 bits: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats; else NULL
+ *   out_scale    8 bits: host array of device pointers to [rows][channels / scale_group] (or [rows]) floats, which alias nothing either; else NULL
  *   run          device, n_tiles bytes, or NULL: all tiles
  * Everything is fp32 between the loads and the stores: y comes from the sum before it is rounded, for every finite s, as in sg_tile_residual_norm.  Mean
  * and variance of SG_NORM_LAYER come from one pass, mean(v^2) - mean(v)^2, where mean^2 <= variance / 4 (which loses less than two bits); of rows farther

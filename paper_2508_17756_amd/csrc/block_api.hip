@@ -29,6 +29,7 @@ class Written {
       if (read[i] >= at_[0] && read[i] <= at_[n_ - 1] && std::binary_search(at_, at_ + n_, read[i]) && !(same_strides && written_[i] == read[i])) return false;
     return true;
   }
+  bool not_at(const void* read) const { return !read || !std::binary_search(at_, at_ + n_, read); }
 
  private:
   void* const* written_;
@@ -178,15 +179,21 @@ int sg_tile_gated_norm(const sg_gated_norm_problem* p, int32_t n_tiles, const vo
     if (list && !tiles_ok(list, n_tiles)) return SG_ERR_INVALID_ARG;
   if (!aligned16(weight) || !aligned16(post_weight)) return SG_ERR_INVALID_ARG;
   if (eight != (out_scale != nullptr) || (eight && !tiles_ok((const void* const*)out_scale, n_tiles, 3u))) return SG_ERR_INVALID_ARG;
+  auto alone = [&](const Written& w) { return w.different() && w.not_at(weight) && w.not_at(post_weight); };
+  auto aliases_nothing = [&](const Written& w) {
+    if (!alone(w) || !w.apart_from(x)) return false;
+    for (const void* const* list : lists)
+      if (!w.apart_from(list)) return false;
+    return w.apart_from((const void* const*)sum);
+  };
   const Written ow(out, n_tiles);
-  if (!ow.different() || !ow.apart_from(x)) return SG_ERR_INVALID_ARG;
-  for (const void* const* list : lists)
-    if (!ow.apart_from(list)) return SG_ERR_INVALID_ARG;
+  if (!aliases_nothing(ow)) return SG_ERR_INVALID_ARG;
+  if (eight && (!aliases_nothing(Written((void* const*)out_scale, n_tiles)) || !ow.apart_from((const void* const*)out_scale))) return SG_ERR_INVALID_ARG;
   if (sum) {
     if (!tiles_ok((const void* const*)sum, n_tiles)) return SG_ERR_INVALID_ARG;
     const Written sw(sum, n_tiles);
-    if (!sw.different() || !sw.apart_from(x, p->x_stride == p->sum_stride) || !sw.apart_from(residual, p->residual_stride == p->sum_stride) ||
-        !sw.apart_from(gate) || !sw.apart_from(scale) || !sw.apart_from(shift) || !ow.apart_from((const void* const*)sum))
+    if (!alone(sw) || !sw.apart_from(x, p->x_stride == p->sum_stride) || !sw.apart_from(residual, p->residual_stride == p->sum_stride) ||
+        !sw.apart_from(gate) || !sw.apart_from(scale) || !sw.apart_from(shift))
       return SG_ERR_INVALID_ARG;
   }
   return launch_gated_norm(*p, n_tiles, x, residual, gate, post_weight, weight, scale, shift, run, sum, out, out_scale, (hipStream_t)stream);
