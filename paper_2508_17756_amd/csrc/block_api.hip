@@ -211,7 +211,8 @@ int sg_tile_int8_linear(const sg_int8_linear_problem* p, int32_t n_tiles, const 
   if (!tiles_ok(x, n_tiles) || !tiles_ok((const void* const*)x_scale, n_tiles, 3u) || !tiles_ok((const void* const*)out, n_tiles)) return SG_ERR_INVALID_ARG;
   if (!w || !aligned16(w) || !w_scale || !aligned16(w_scale) || !aligned16(bias)) return SG_ERR_INVALID_ARG;
   const Written ow(out, n_tiles);
-  if (!ow.different() || !ow.apart_from(x)) return SG_ERR_INVALID_ARG;
+  if (!ow.different() || !ow.apart_from(x) || !ow.apart_from((const void* const*)x_scale) || !ow.not_at(w) || !ow.not_at(w_scale) || !ow.not_at(bias))
+    return SG_ERR_INVALID_ARG;
   // rows are numbered in 31 bits; the largest calls are cut into blocks of 256 x 256, a workgroup of 512 threads each, for 64 tiles a launch
   const int64_t rows = (int64_t)p->rows * std::min(n_tiles, 64);
   if ((int64_t)p->rows * n_tiles >= (1ll << 31) || (rows + 255) / 256 * ((p->outputs + 255ll) / 256) >= (1ll << 23)) return SG_ERR_UNSUPPORTED;

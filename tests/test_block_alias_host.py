@@ -1,7 +1,7 @@
-"""Buffers that gated norms write and that are written or read in another place too are refused, on the host (no GPU is touched here)."""
+"""Buffers that gated norms and 8-bit integer linear layers write and that are written or read in another place too are refused, on the host (no GPU is touched here)."""
 import pytest
 
-from test_block_host import BAD, DONE, GOOD, _norm, no_device
+from test_block_host import BAD, DONE, GOOD, _at, _linear, _list, _norm, no_device
 
 EIGHT = {"out_dtype": 3}
 PLACE = GOOD + 4096 * 50   # in nobody's list unless it is put there
@@ -26,3 +26,15 @@ def test_norms_whose_buffers_lie_apart():
     assert _norm(fields=EIGHT, out_scale=[700, 701], weight=PLACE, post_weight=PLACE) == DONE
     assert _norm(fields=EIGHT, out_scale=[700, 701], total=[0, 1]) == DONE
     assert _norm(out_scale=None, total=[100, 101], weight=PLACE) == DONE
+
+
+@pytest.mark.parametrize("kw", [dict(x_scale=_list([600, 301])), dict(x_scale=_list([300, 600])), dict(w=PLACE, out=_list([600, 50])), dict(w_scale=PLACE, out=_list([50, 601])),
+                                dict(bias=PLACE, out=_list([50, 601]))])
+def test_linear_results_in_a_place_that_is_read(kw):
+    assert _linear(**kw) == BAD
+
+
+@no_device
+def test_linear_results_that_lie_apart():
+    assert _linear(w=PLACE, w_scale=PLACE, bias=PLACE) == DONE
+    assert _linear(x_scale=_at(2, 300), bias=None, out=_list([50, 51])) == DONE
