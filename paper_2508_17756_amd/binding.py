@@ -7,6 +7,7 @@ been built, loading raises.
 """
 import ctypes
 import os
+import struct
 
 SG_F32, SG_BF16, SG_F8_E4M3, SG_I8 = 0, 1, 2, 3
 SG_OK, SG_ERR_INVALID_ARG, SG_ERR_UNSUPPORTED, SG_ERR_WORKSPACE, SG_ERR_HIP = 0, -1, -2, -3, -4
@@ -207,13 +208,14 @@ def load_library():
     lib.sg_rotary_frequencies.argtypes = [rot, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                           ctypes.POINTER(ctypes.c_double)]
     lib.sg_tile_rotary.restype = ctypes.c_int
-    lib.sg_tile_rotary.argtypes = [rot, i32, pp, pp, vp, ctypes.POINTER(i32), pp, vp, vp, vp, pp, pp, vp]
+    # (lists of addresses as _tiles packs them)
+    lib.sg_tile_rotary.argtypes = [rot, i32, vp, vp, vp, ctypes.POINTER(i32), vp, vp, vp, vp, vp, vp, vp]
     lib.sg_tile_gated_norm.restype = ctypes.c_int
-    lib.sg_tile_gated_norm.argtypes = [ctypes.POINTER(sg_gated_norm_problem), i32, pp, pp, pp, vp, vp, pp, pp, vp, pp, pp, pp, vp]
+    lib.sg_tile_gated_norm.argtypes = [ctypes.POINTER(sg_gated_norm_problem), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.sg_int8_linear_validate.restype = ctypes.c_int
     lib.sg_int8_linear_validate.argtypes = [ctypes.POINTER(sg_int8_linear_problem)]
     lib.sg_tile_int8_linear.restype = ctypes.c_int
-    lib.sg_tile_int8_linear.argtypes = [ctypes.POINTER(sg_int8_linear_problem), i32, pp, pp, vp, vp, vp, vp, pp, vp]
+    lib.sg_tile_int8_linear.argtypes = [ctypes.POINTER(sg_int8_linear_problem), i32, vp, vp, vp, vp, vp, vp, vp, vp]
     _LIB = lib
     return lib
 
@@ -587,18 +589,6 @@ def _vector(t, kinds, n, name):
     return t.data_ptr()
 
 
-def _vectors(tensors, kind, n, elements, name):
-    """_pointers of device arrays of `elements` each, checked as _vector does."""
-    if len(tensors) != n:
-        raise ValueError("%d tensors for %d tiles" % (len(tensors), n))
-    at = []
-    for t in tensors:
-        if t.dtype is not kind or t.numel() < elements or not t.is_cuda or not t.is_contiguous():
-            _vector(t, (kind,), elements, name)
-        at.append(t.data_ptr())
-    return (ctypes.c_void_p * (n or 1))(*at)
-
-
 def _lengths(t, n, name):
     return None if t is None else _vector(t, (_torch().int32,), n, name)
 
@@ -645,6 +635,70 @@ def sg_tile_residual_norm(p, x, weight, out, residual=None, sum_out=None, out_sc
 
 
 # ------------------------------------------------------------------ rotary positions, gated norm, 8-bit integer linear layer
+_KINDS = {}
+
+
+def _kind(code):
+    """The torch type of the tensors that an sg_dtype stands for; None for a number that is no such type (which the library refuses)."""
+    if not _KINDS:
+        torch = _torch()
+        _KINDS.update({SG_F32: torch.float32, SG_BF16: torch.bfloat16, SG_F8_E4M3: torch.float8_e4m3fn, SG_I8: torch.int8})
+    return _KINDS.get(code)
+
+
+class _Packers(dict):
+    """n addresses -> the list of them that the library reads."""
+
+    def __missing__(self, n):
+        self[n] = pack = struct.Struct("%dQ" % n).pack
+        return pack
+
+
+_PACK = _Packers()
+
+
+def _tiles(tensors, kind, n, name):
+    """The addresses of one tensor for each of n tiles, as the library reads a list; NULL for no list.  Tensors of another type would be read as this one, or
+    written past their end, without a word."""
+    if tensors is None:
+        return None
+    at = [t.data_ptr() for t in tensors if t.dtype is kind]
+    if len(at) != n or len(tensors) != n:
+        at = _others(tensors, kind, n, name)
+    return _PACK[n](*at)
+
+
+def _others(tensors, kind, n, name):
+    """_tiles of a list that is not n tensors of one kind."""
+    if len(tensors) != n:
+        raise ValueError("%d tensors for %d tiles" % (len(tensors), n))
+    torch = _torch()
+    kinds = (kind, torch.uint8) if kind is torch.float8_e4m3fn else (kind,)   # (the bits of the 8-bit values)
+    for t in tensors:
+        if kind is not None and t.dtype not in kinds:
+            raise TypeError("%s must be %s, not %s" % (name, " or ".join(str(k) for k in kinds), t.dtype))
+    return [t.data_ptr() for t in tensors]
+
+
+def _vectors(tensors, kind, n, elements, name, packed=True):
+    """_tiles of device arrays of `elements` elements each, checked as _vector does; packed: without gaps."""
+    if tensors is None:
+        return None
+    at = [t.data_ptr() for t in tensors if t.dtype is kind and t.numel() >= elements and t.is_cuda and (not packed or t.is_contiguous())]
+    if len(at) != n or len(tensors) != n:
+        at = _others(tensors, kind, n, name)
+        for t in tensors:
+            if t.numel() < elements or (packed and not t.is_contiguous()):
+                raise ValueError("%s must %shold %d elements" % (name, "be contiguous and " if packed else "", elements))
+            if not t.is_cuda:
+                raise ValueError("%s must be in device memory" % name)
+    return _PACK[n](*at)
+
+
+def _weight(t, kind, n, name):
+    return None if t is None else _vector(t, (t.dtype if kind is None else kind,), n, name)
+
+
 _LAYOUTS = {"interleaved": SG_ROTARY_INTERLEAVED, "half": SG_ROTARY_HALF}
 _SCALINGS = {"none": SG_ROTARY_PLAIN, "linear": SG_ROTARY_LINEAR, "ntk": SG_ROTARY_NTK, "ramp": SG_ROTARY_RAMP}
 _NORMS = {"none": SG_NORM_NONE, "rms": SG_NORM_RMS, "layer": SG_NORM_LAYER}
@@ -691,10 +745,11 @@ def sg_tile_rotary(p, q, q_out, frequencies, k=None, k_out=None, origin=None, po
         if len(origin) != n:
             raise ValueError("%d origins for %d tiles" % (len(origin), n))
         at = (ctypes.c_int32 * (3 * n or 1))(*[int(v) for o in origin for v in (o[0], o[1], o[2])])
-    listed = None if positions is None else _vectors(positions, torch.int32, n, p.T * p.H * p.W * p.position_axes, "positions")
-    st = load_library().sg_tile_rotary(ctypes.byref(p), n, _ptr_array(q), _pointers(k, n), _vector(frequencies, (torch.float64,), pairs, "frequencies"), at,
-                                       listed, _ptr(q_weight), _ptr(k_weight), _flags(run, n, "run"), _pointers(q_out, n),
-                                       _pointers(k_out, n), _stream())
+    kind = _kind(p.dtype)
+    listed = _vectors(positions, torch.int32, n, p.T * p.H * p.W * p.position_axes, "positions")
+    st = load_library().sg_tile_rotary(ctypes.byref(p), n, _tiles(q, kind, n, "q"), _tiles(k, kind, n, "k"), _vector(frequencies, (torch.float64,), pairs, "frequencies"),
+                                       at, listed, _weight(q_weight, kind, p.head_dim, "q_weight"), _weight(k_weight, kind, p.head_dim, "k_weight"),
+                                       _flags(run, n, "run"), _tiles(q_out, kind, n, "q_out"), _tiles(k_out, kind, n, "k_out"), _stream())
     _check(st, "sg_tile_rotary")
     return q_out if k is None else (q_out, k_out)
 
@@ -715,10 +770,15 @@ def sg_tile_gated_norm(p, x, out, residual=None, gate=None, post_weight=None, we
                        run=None):
     """x, out, residual, gate, scale, shift, sum_out, out_scale: lists of one tensor per tile, all but the first two or None; post_weight, weight:
     `channels` elements or None; run: uint8 or bool."""
-    n = len(x)
-    st = load_library().sg_tile_gated_norm(ctypes.byref(p), n, _ptr_array(x), _pointers(residual, n), _pointers(gate, n), _ptr(post_weight),
-                                           _ptr(weight), _pointers(scale, n), _pointers(shift, n), _flags(run, n, "run"), _pointers(sum_out, n),
-                                           _pointers(out, n), _pointers(out_scale, n), _stream())
+    n, c = len(x), p.channels
+    kind, mods = _kind(p.dtype), _kind(p.mod_dtype)
+    mod = c * (-(-p.rows // p.mod_rows) if 0 < p.mod_rows < p.rows else 1)
+    groups = c // p.scale_group if p.scale_group > 0 else 1
+    st = load_library().sg_tile_gated_norm(
+        ctypes.byref(p), n, _tiles(x, kind, n, "x"), _tiles(residual, kind, n, "residual"), _vectors(gate, mods, n, mod, "gate", False),
+        _weight(post_weight, kind, c, "post_weight"), _weight(weight, kind, c, "weight"), _vectors(scale, mods, n, mod, "scale", False),
+        _vectors(shift, mods, n, mod, "shift", False), _flags(run, n, "run"), _tiles(sum_out, kind, n, "sum_out"), _tiles(out, _kind(p.out_dtype), n, "out"),
+        _vectors(out_scale, _kind(SG_F32), n, p.rows * groups, "out_scale"), _stream())
     _check(st, "sg_tile_gated_norm")
     return out
 
@@ -735,13 +795,12 @@ def sg_int8_linear_validate(p):
 
 def sg_tile_int8_linear(p, x, x_scale, w, w_scale, out, bias=None, run=None):
     """x (int8), x_scale (float32), out: lists of one tensor per tile; w: int8; w_scale: float32; bias: `outputs` elements or None; run: uint8 or bool."""
-    n, torch = len(x), _torch()
-    int8 = torch.int8
-    for t in (w, *x):
-        if t.dtype is not int8:
-            raise TypeError("x and w must be torch.int8, not %s" % t.dtype)
-    st = load_library().sg_tile_int8_linear(ctypes.byref(p), n, _ptr_array(x), _vectors(x_scale, torch.float32, n, p.rows, "x_scale"), _ptr(w),
-                                            _vector(w_scale, (torch.float32,), p.outputs, "w_scale"), _ptr(bias), _flags(run, n, "run"),
-                                            _pointers(out, n), _stream())
+    n, f32, int8 = len(x), _kind(SG_F32), _kind(SG_I8)
+    rows, scales = _tiles(x, int8, n, "x"), _vectors(x_scale, f32, n, p.rows, "x_scale")
+    if w.dtype is not int8 or w.numel() < p.outputs * p.channels or not w.is_cuda:
+        _vectors((w,), int8, 1, p.outputs * p.channels, "w", False)   # (says what is wrong)
+    st = load_library().sg_tile_int8_linear(ctypes.byref(p), n, rows, scales, _ptr(w), _vector(w_scale, (f32,), p.outputs, "w_scale"),
+                                            _weight(bias, _kind(p.dtype), p.outputs, "bias"),
+                                            _flags(run, n, "run"), _tiles(out, _kind(p.dtype), n, "out"), _stream())
     _check(st, "sg_tile_int8_linear")
     return out
