@@ -574,7 +574,8 @@ int sg_rotary_validate(const sg_rotary_problem* p);
  * Frequencies of the R / 2 pairs in radians per position (host only; `out` is host memory, what sg_tile_rotary reads a device copy of it):
  * base^(-2 i / n) for pair i of an axis of n channels, and then
  *   SG_ROTARY_LINEAR   divided by factor
- *   SG_ROTARY_NTK      of base * factor^(n / (n - 2)) in the place of base: the last pair of an axis is divided by factor, the first stays
+ *   SG_ROTARY_NTK      of base * factor^(n / (n - 2)) in the place of base: the last pair of an axis is divided by factor, the first stays (so does the only
+ *                      pair of an axis of 2 channels)
  *   SG_ROTARY_RAMP     pairs that turn `fast` times or more over `length` positions stay, those that turn `slow` times or less are divided by factor,
  *                      and between them the part that stays grows in proportion
  * base > 0, factor > 0, length > 0, 0 <= slow < fast, all finite (factor, length, slow, fast: where the scaling uses them).

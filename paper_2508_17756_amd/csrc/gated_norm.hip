@@ -3,8 +3,8 @@
 // in the tensors' type or in 8 bits with scales.  Everything between the loads and the stores is fp32 and stays in registers: one read of x and the
 // residual, one write of s and out.  Bound by memory.
 //
-// 75,600 rows of 5,120, bf16, layer norm with gate, scale and shift to e4m3 483 us (5.6 TB/s; a large copy runs at 4.9), with those in fp32 613; 4 tiles of
-// 2,925 rows of 1,536 with a norm of x and fp32 vectors for each 225 rows 34 us (4.2); 10^6 rows of 128 186 us (5.5).
+// 75,600 rows of 5,120, bf16, layer norm with gate, scale and shift to e4m3 477 us (5.7 TB/s; a large copy runs at 4.9), with those in fp32 603; 4 tiles of
+// 2,925 rows of 1,536 with a norm of x and fp32 vectors for each 225 rows 35 us (4.1); 10^6 rows of 128 190 us (5.4).
 //
 // What keeps it from the memory's rate is the arithmetic beside it (some 550 vector instructions for 24 channels of a wavefront, half of the time) and the
 // chain of latencies of a row: loads, one or two reductions, loads of what the reductions stand in front of, stores.  So a lane holds 3 vectors of 8
@@ -441,9 +441,9 @@ int launch_gated_norm(const sg_gated_norm_problem& p, int n_tiles, const void* c
   a.has_sum = sum != nullptr;
   a.residual_scale = p.residual_scale; a.eps = p.eps; a.post_eps = p.post_eps;
   a.by_channels = 1.f / (float)p.channels;
-  // Up to 256 channels rows share a wavefront, 2 vectors a lane (10^6 rows of 128 channels 186 us, one vector 343 in an earlier form; with blocks of 128 channels always one,
-  // which leaves a block to 16 lanes side by side).  512 channels: one wavefront with one vector a lane (400,000 rows 270 us; shared 313).  Then up to 3
-  // vectors; beyond 6,144 channels 2 (30,000 rows of 8,192 340 us; 3: 450) up to 16 wavefronts and beyond 16,384 4.
+  // Up to 256 channels rows share a wavefront, 2 vectors a lane (10^6 rows of 128 channels 190 us, one vector 343 in an earlier form; with blocks of 128 channels always one,
+  // which leaves a block to 16 lanes side by side).  512 channels: one wavefront with one vector a lane (400,000 rows 256 us; shared 313 when that took 270).  Then up to 3
+  // vectors; beyond 6,144 channels 2 (30,000 rows of 8,192 324 us; 3: 450 when that took 340) up to 16 wavefronts and beyond 16,384 4.
   const bool is_short = a.n_vec <= 32;
   int vpl, threads = 256;
   if (is_short) {
@@ -479,7 +479,7 @@ int launch_gated_norm(const sg_gated_norm_problem& p, int n_tiles, const void* c
     a.n_rows = (uint32_t)n * (uint32_t)p.rows;
     a.run = run ? run + t0 : nullptr;
     uint32_t grid = (a.n_rows + rows_per_wg - 1) / rows_per_wg;
-    // New workgroups for new rows: walking them, 2,048 workgroups took 344 us instead of 205 for 10^6 rows of 128 channels.  (2^21 a launch, then they walk.)
+    // New workgroups for new rows: walking them, 2,048 workgroups took 344 us instead of 205 for 10^6 rows of 128 channels (190 by now).  (2^21 a launch, then they walk.)
     if (grid > 1u << 21) grid = 1u << 21;
     const int st = p.dtype == SG_F32      ? launch<float, float>(a, tab, is_short, vpl, threads, grid, s)
                    : p.mod_dtype == SG_F32 ? launch<uint16_t, float>(a, tab, is_short, vpl, threads, grid, s)

@@ -7,8 +7,8 @@
 // w is the instruction's first operand, its rows in an order that leaves a lane with outputs side by side of one row, which it scales and stores together.
 //
 // Large calls: held in registers, N(0, 32)-distributed integers pass the instruction at 3.9 POP/s, bound by power (zeros: 4.9; the form 32x32x32, which touches each
-// sum twice as often, at 3.3).  Blocks of 256 x 256: 34,560 x 5,120 x 15,360 2.15 - 2.19 ms = 2.48 - 2.53 POP/s (all zeros: 1.74 ms), 75,600 x 5,120 x 20,480 with GELU
-// 6.6 - 6.8 ms.  A block's 40 stages take seven eighths of its time, its start and its stores the last.  What the stages lose, timed with parts left out, are
+// sum twice as often, at 3.3).  Blocks of 256 x 256: 34,560 x 5,120 x 15,360 2.13 - 2.19 ms = 2.48 - 2.55 POP/s (all zeros: 1.74 ms), 75,600 x 5,120 x 20,480 with GELU
+// 6.6 - 6.9 ms.  A block's 40 stages take seven eighths of its time, its start and its stores the last.  What the stages lose, timed with parts left out, are
 // the loads from the L2 into LDS (64 KiB a stage; without them 1.76 ms, zeros 1.43), hardly the barriers (a further 0.02) and not the reads of LDS.
 // 32x32x32 instead: 2.58 ms at the first size; all of a stage's loads behind its barrier: 2.23; factors and places of the rows looked up at the end: 2.35.
 #include <atomic>
@@ -76,7 +76,8 @@ __device__ __forceinline__ int running_tiles(const LinearArgs& a, int* list) {
 }
 
 // Workgroups go to the 8 XCDs in turn: each XCD takes a run of blocks, in columns of up to 4 blocks of rows, so that the 32 that run on it side by
-// side share 4 parts of x and 8 of w in its L2 (75,600 x 5,120 x 20,480: 6.77 ms; columns of 8 6.95, of 16 7.10).
+// side share 4 parts of x and 8 of w in its L2 (75,600 x 5,120 x 20,480: 6.77 ms; columns of 8 6.95, of 16 7.10).  The runs are of all rows of the call: where tiles do not run, the blocks that are left meet
+// on the first XCDs (9 tiles of 3,840 x 5,120 x 15,360 2.13 ms, 4 of them 1.96, one 1.64).
 __device__ __forceinline__ void block_of(uint32_t id, uint32_t gm, uint32_t gn, uint32_t& m, uint32_t& n) {
   const uint32_t all = gm * gn, xcd = id & 7, per = all >> 3, more = all & 7;
   const uint32_t at = xcd * per + (xcd < more ? xcd : more) + (id >> 3);
